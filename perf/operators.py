@@ -91,7 +91,7 @@ def _round(x, format):
         t = e - 3 + (m > 0.75)                  # 6 = .75 * 2^3
     else:
         t = e - 9 + (m > 0.875)                 # 448 = .875 * 2^9
-    t = torch.where(m == 0, -127, t.clamp(-127, 127))
+    t = torch.where(m == 0, -126, t.clamp(-126, 127))
     a = torch.ldexp(v, -t)
     size = a.abs()
     if format == "mxfp4":
@@ -409,7 +409,7 @@ def _nearest(x, format):
         t = torch.ceil(torch.log2(top / grid[-1]))
         t = torch.where(torch.exp2(t - 1) * grid[-1] >= top, t - 1, t)           # (the logarithm is rounded: its neighbours are looked at)
         t = torch.where(torch.exp2(t) * grid[-1] < top, t + 1, t)
-        s = torch.exp2(torch.where(top > 0, t, torch.zeros_like(t)).clamp(-127, 127))
+        s = torch.exp2(torch.where(top > 0, t, torch.zeros_like(t)).clamp(-126, 127))
         u = (v / s).abs()
         up = torch.searchsorted(grid, u).clamp(max=grid.shape[0] - 1)            # the first value that is not below it
         down = (up - 1).clamp(min=0)
