@@ -46,6 +46,7 @@ typedef enum {
 
 typedef enum { PK_F32 = 0, PK_BF16 = 1 } pk_dtype;
 typedef enum { PK_SUM = 0, PK_MEAN = 1 } pk_pool;
+typedef enum { PK_MXFP4 = 0, PK_MXFP8 = 1 } pk_mx_format;   /* microscaled rows, see pk_mx_quantize */
 
 /* One embedding table: rows x dim elements of dtype. */
 typedef struct { int64_t rows; int32_t dim; int32_t dtype; } pk_table_desc;
@@ -299,6 +300,78 @@ size_t    pk_partition_scratch_bytes(const pk_plan* plan, int64_t nnz, int32_t n
 pk_status pk_partition_unique(const pk_plan* plan, const void* workspace, size_t ws_bytes, int32_t B, int64_t nnz,
                               int32_t p, int32_t n_owners, uint32_t* part_keys, int32_t* part_index,
                               int32_t* part_offsets, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/* ---- microscaled rows: tables and activations in 4 and 8 bits ------------------
+ * A row of `cols` numbers is cut into blocks of 32 columns (the last one may be
+ * shorter).  A block has one scale 2^t, t the smallest integer, -126 at least, with
+ * which the block's largest magnitude is at most 2^t times the format's largest
+ * value; its elements divided by 2^t are rounded to the nearest value of the format,
+ * ties to the even code, so that an element of a block is off by at most half a step:
+ *   PK_MXFP4  E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; two columns a byte, the
+ *             lower column in the lower bits
+ *   PK_MXFP8  E4M3: sign, four exponent and three mantissa bits, up to 448; a byte each
+ * (the element and scale formats are those of the OCP microscaling formats).
+ * A row in memory: the codes in whole 4-byte words (behind the last column zeros),
+ * then a byte t + 127 per block, then zeros up to a whole word.  A block that holds an
+ * infinity or a NaN gets the scale byte 255, and all its columns read back as NaN.
+ * Rows and row_stride (bytes) are multiples of 4, row_stride >= pk_mx_row_bytes; bytes
+ * of the stride behind the row are neither read nor written.  Rows whose address and
+ * stride are multiples of 16 are read faster by pk_mx_linear and pk_mx_weight_grad.
+ *
+ * Matrices of fp32 or bf16: element-aligned, row stride in elements, >= the columns
+ * (not looked at for one row).  Sizes below 2^31.  Calls with no rows do nothing
+ * (pk_mx_weight_grad: the sum over no samples).  These calls need no plan, allocate
+ * nothing and only enqueue work on hip_stream, which belongs to the current device;
+ * workspaces are the caller's, and calls that may run at the same time (two streams,
+ * two graphs) need one each. */
+size_t    pk_mx_row_bytes(int32_t format, int64_t cols);   /* 0: unknown format or bad cols */
+/* src: device, fp32 or bf16 [n_rows, src_row_stride]; rows: device, out. */
+pk_status pk_mx_quantize(const void* src, int32_t src_dtype, int64_t src_row_stride, int64_t n_rows, int64_t cols,
+                         int32_t format, void* rows, int64_t row_stride, void* hip_stream);
+/* dst: device, fp32 or bf16 [n_rows, dst_row_stride], columns [0, cols) are written.
+ * Both types hold every value of both formats exactly (bf16: from 2^-133 on). */
+pk_status pk_mx_dequantize(const void* rows, int64_t row_stride, int64_t n_rows, int64_t cols, int32_t format,
+                           void* dst, int32_t dst_dtype, int64_t dst_row_stride, void* hip_stream);
+
+/* The pooled lookup of pk_forward (Gather, SegmentReduction) from tables held in
+ * 4 bits, for serving: no Unique, no context, no workspace, nothing to go backward.
+ * T:        host array of n_packs DEVICE pointers, 4-byte aligned; T[p] holds pack p's
+ *           stacked table, total_rows rows of PK_MXFP4 with row_stride =
+ *           pk_mx_row_bytes(PK_MXFP4, dim).  The plan's dtypes say what the tables were
+ *           rounded from.
+ * ids, offsets, out: as for pk_forward; sums are kept in double, the mean's division too.
+ * error_word: device, int32.  Offsets that violate the contract raise bit 0 (OR: the
+ *           caller clears it); a bag that begins before 0, ends before it begins or
+ *           behind nnz pools to zeros, nothing is read for it, and the others are pooled. */
+pk_status pk_mx_forward(const pk_plan* plan, const void* const* T, const int64_t* ids, const int32_t* offsets,
+                        int32_t B, int64_t nnz, float* out, int64_t out_row_stride, int32_t* error_word,
+                        void* hip_stream);
+
+/* The dense layer behind the pooled output, in 4 bits:
+ *   y[m, n] = bias[n] + sum_k Q(x)[m, k] * W[n, k]
+ * Q(x): x rounded to PK_MXFP4 rows in this call; sums in fp32, y rounded once.
+ * x: device, fp32 or bf16 [M, x_row_stride];  w_rows: device, N rows of K columns, PK_MXFP4;
+ * bias: device, fp32 [N] or NULL;  y: device, fp32 or bf16 [M, y_row_stride].
+ * workspace: device, 256-byte aligned, >= pk_mx_linear_workspace_bytes(M, N, K) (which is
+ * 0 for bad sizes).  A NaN in x makes its whole row of y NaN, one in W its column. */
+size_t    pk_mx_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int64_t M,
+                       const void* w_rows, int64_t w_row_stride, int64_t N, int64_t K, const float* bias,
+                       void* y, int32_t y_dtype, int64_t y_row_stride,
+                       void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* The gradient of a dense layer's weights from the 8-bit checkpoint of its input:
+ *   dw[n, k] (+)= sum_b dy[b, n] * X[b, k]
+ * dy: device, fp32 or bf16 [B, dy_row_stride] (fp32 numbers are multiplied in full);
+ * x_rows: device, B rows of K columns, PK_MXFP8;  dw: device, fp32 [N, dw_row_stride].
+ * accumulate: 0 = dw is overwritten, else added to (micro-batches).  Sums in fp32, in an
+ * order that depends on the sizes only: the same call gives the same bits.
+ * workspace: device, 256-byte aligned, >= pk_mx_weight_grad_workspace_bytes(B, N, K). */
+size_t    pk_mx_weight_grad_workspace_bytes(int64_t B, int64_t N, int64_t K);
+pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_stride,
+                            const void* x_rows, int64_t x_row_stride, int64_t B, int64_t N, int64_t K,
+                            float* dw, int64_t dw_row_stride, int32_t accumulate,
+                            void* workspace, size_t ws_bytes, void* hip_stream);
 
 /* ---- parity access to the context saved in the workspace ---------------------
  * SYNCHRONISES the device (copies a few bytes of the header back).  Returns

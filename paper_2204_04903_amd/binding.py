@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libpk.so")
 PK_OK, PK_EINVAL, PK_ESHAPE, PK_EWORKSPACE, PK_EOVERFLOW, PK_EHIP, PK_ENOMEM = range(7)
 PK_F32, PK_BF16 = 0, 1
 PK_SUM, PK_MEAN = 0, 1
+PK_MXFP4, PK_MXFP8 = 0, 1
 
 EXPORTS = [
     "pk_plan_create", "pk_plan_destroy", "pk_plan_num_packs", "pk_plan_pack_info", "pk_plan_pack_fields",
@@ -27,6 +28,8 @@ EXPORTS = [
     "pk_hh_scratch_bytes", "pk_hh_init", "pk_hh_forward", "pk_hh_backward_update", "pk_hh_end_iteration",
     "pk_hh_hot_count", "pk_forward_dedup", "pk_forward_pool", "pk_micro_batch_size", "pk_forward_static",
     "pk_partition_scratch_bytes", "pk_partition_unique",
+    "pk_mx_row_bytes", "pk_mx_quantize", "pk_mx_dequantize", "pk_mx_forward", "pk_mx_linear_workspace_bytes", "pk_mx_linear",
+    "pk_mx_weight_grad_workspace_bytes", "pk_mx_weight_grad",
 ]
 
 
@@ -58,7 +61,8 @@ class PkError(RuntimeError):
 
 def build(force: bool = True) -> str:
     """Compile the library for gfx950 (hipcc cross-compiles without a GPU)."""
-    src = [os.path.join(_HERE, "csrc", "pk_plan.cpp"), os.path.join(_HERE, "csrc", "pk_device.hip")]
+    src = [os.path.join(_HERE, "csrc", "pk_plan.cpp"), os.path.join(_HERE, "csrc", "pk_device.hip"),
+           os.path.join(_HERE, "csrc", "pk_mx.hip")]
     deps = src + [os.path.join(_HERE, "csrc", f) for f in sorted(os.listdir(os.path.join(_HERE, "csrc")))
                   if f.endswith(".h")] + [os.path.join(_ROOT, "include", "pk.h")]
     if not force and os.path.exists(LIB_PATH) and all(os.path.getmtime(LIB_PATH) >= os.path.getmtime(d) for d in deps):
@@ -143,6 +147,23 @@ def lib():
                                           ctypes.POINTER(i64), ctypes.POINTER(i64), ctypes.POINTER(i32)]
         L.pk_hh_hot_count.restype = ctypes.c_int
         L.pk_hh_hot_count.argtypes = [vp, i32, ctypes.POINTER(i64)]
+        sz = ctypes.c_size_t
+        L.pk_mx_row_bytes.restype = sz
+        L.pk_mx_row_bytes.argtypes = [i32, i64]
+        L.pk_mx_quantize.restype = ctypes.c_int
+        L.pk_mx_quantize.argtypes = [vp, i32, i64, i64, i64, i32, vp, i64, vp]
+        L.pk_mx_dequantize.restype = ctypes.c_int
+        L.pk_mx_dequantize.argtypes = [vp, i64, i64, i64, i32, vp, i32, i64, vp]
+        L.pk_mx_forward.restype = ctypes.c_int
+        L.pk_mx_forward.argtypes = [vp, ctypes.POINTER(vp), vp, vp, i32, i64, vp, i64, vp, vp]
+        L.pk_mx_linear_workspace_bytes.restype = sz
+        L.pk_mx_linear_workspace_bytes.argtypes = [i64, i64, i64]
+        L.pk_mx_linear.restype = ctypes.c_int
+        L.pk_mx_linear.argtypes = [vp, i32, i64, i64, vp, i64, i64, i64, vp, vp, i32, i64, vp, sz, vp]
+        L.pk_mx_weight_grad_workspace_bytes.restype = sz
+        L.pk_mx_weight_grad_workspace_bytes.argtypes = [i64, i64, i64]
+        L.pk_mx_weight_grad.restype = ctypes.c_int
+        L.pk_mx_weight_grad.argtypes = [vp, i32, i64, vp, i64, i64, i64, i64, vp, i64, i32, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -332,6 +353,55 @@ def pk_hh_hot_count(plan: int, p: int) -> int:
     n = ctypes.c_int64()
     _check(lib().pk_hh_hot_count(plan, p, ctypes.byref(n)))
     return n.value
+
+
+def _size(n: int) -> int:
+    if n == 0:
+        raise PkError(PK_EINVAL, pk_last_error())
+    return int(n)
+
+
+def pk_mx_row_bytes(format: int, cols: int) -> int:
+    n = int(lib().pk_mx_row_bytes(format, cols))
+    if n == 0:
+        raise PkError(PK_EINVAL, "pk_mx_row_bytes: unknown format or bad cols")
+    return n
+
+
+def pk_mx_quantize(src, src_dtype: int, src_row_stride: int, n_rows: int, cols: int, format: int, rows, row_stride: int,
+                   stream: int = 0) -> None:
+    _check(lib().pk_mx_quantize(_ptr(src), src_dtype, src_row_stride, n_rows, cols, format, _ptr(rows), row_stride, stream))
+
+
+def pk_mx_dequantize(rows, row_stride: int, n_rows: int, cols: int, format: int, dst, dst_dtype: int, dst_row_stride: int,
+                     stream: int = 0) -> None:
+    _check(lib().pk_mx_dequantize(_ptr(rows), row_stride, n_rows, cols, format, _ptr(dst), dst_dtype, dst_row_stride, stream))
+
+
+def pk_mx_forward(plan: int, T: Sequence, ids, offsets, B: int, nnz: int, out, out_row_stride: int, error_word,
+                  stream: int = 0) -> None:
+    _check(lib().pk_mx_forward(plan, _ptr_array(T), _ptr(ids), _ptr(offsets), B, nnz, _ptr(out), out_row_stride,
+                               _ptr(error_word), stream))
+
+
+def pk_mx_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return _size(lib().pk_mx_linear_workspace_bytes(M, N, K))
+
+
+def pk_mx_linear(x, x_dtype: int, x_row_stride: int, M: int, w_rows, w_row_stride: int, N: int, K: int, bias, y, y_dtype: int,
+                 y_row_stride: int, workspace, ws_bytes: int, stream: int = 0) -> None:
+    _check(lib().pk_mx_linear(_ptr(x), x_dtype, x_row_stride, M, _ptr(w_rows), w_row_stride, N, K, _ptr(bias), _ptr(y), y_dtype,
+                              y_row_stride, _ptr(workspace), ws_bytes, stream))
+
+
+def pk_mx_weight_grad_workspace_bytes(B: int, N: int, K: int) -> int:
+    return _size(lib().pk_mx_weight_grad_workspace_bytes(B, N, K))
+
+
+def pk_mx_weight_grad(dy, dy_dtype: int, dy_row_stride: int, x_rows, x_row_stride: int, B: int, N: int, K: int, dw,
+                      dw_row_stride: int, accumulate: bool, workspace, ws_bytes: int, stream: int = 0) -> None:
+    _check(lib().pk_mx_weight_grad(_ptr(dy), dy_dtype, dy_row_stride, _ptr(x_rows), x_row_stride, B, N, K, _ptr(dw),
+                                   dw_row_stride, 1 if accumulate else 0, _ptr(workspace), ws_bytes, stream))
 
 
 def pk_ctx_pack(plan: int, workspace, B: int, nnz: int, p: int) -> dict:

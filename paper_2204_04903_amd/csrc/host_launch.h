@@ -246,8 +246,7 @@ struct Ws {
     template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(base + off); }
 };
 
-pk_status check_common(const pk_plan* plan, int32_t B, int64_t nnz, const void* ws, size_t ws_bytes, const char* who,
-                       size_t room = ~(size_t)0)
+pk_status check_batch(const pk_plan* plan, int32_t B, int64_t nnz, const char* who)
 {
     if (!plan) return fail(PK_EINVAL, std::string(who) + ": plan is NULL");
     if (B <= 0) return fail(PK_ESHAPE, std::string(who) + ": B must be positive");
@@ -257,6 +256,14 @@ pk_status check_common(const pk_plan* plan, int32_t B, int64_t nnz, const void* 
     if (plan->opts.max_nnz > 0 && nnz > plan->opts.max_nnz) return fail(PK_ESHAPE, std::string(who) + ": nnz exceeds the plan's max_nnz");
     if ((int64_t)B * plan->out_dim >= ((int64_t)1 << 32)) return fail(PK_EOVERFLOW, std::string(who) + ": B * out_dim must be below 2^32");
     if ((int64_t)B * (int64_t)plan->fields.size() >= ((int64_t)1 << 31)) return fail(PK_EOVERFLOW, std::string(who) + ": n_fields * B must be below 2^31");
+    return PK_OK;
+}
+
+pk_status check_common(const pk_plan* plan, int32_t B, int64_t nnz, const void* ws, size_t ws_bytes, const char* who,
+                       size_t room = ~(size_t)0)
+{
+    const pk_status rc = check_batch(plan, B, nnz, who);
+    if (rc != PK_OK) return rc;
     if (!ws) return fail(PK_EINVAL, std::string(who) + ": workspace is NULL");
     if (reinterpret_cast<uintptr_t>(ws) % kAlign) return fail(PK_EWORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
     if (ws_bytes < make_layout(plan, B, nnz, room).total) return fail(PK_EWORKSPACE, std::string(who) + ": workspace is smaller than pk_workspace_bytes");

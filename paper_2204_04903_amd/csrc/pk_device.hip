@@ -48,6 +48,8 @@ static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes + kSt
 //   dev_small.h    H1 and H2 of small batches
 //   dev_rows.h     row access, plain or hybrid row addressing
 //   dev_pool.h     pooling (H3-H5) and the one launch of the forward pass for small batches
+//   dev_mx.h       microscaled numbers (shared with pk_mx.hip)
+//   dev_mx_lookup.h  pooled lookup from tables of microscaled 4-bit rows
 //   dev_adagrad.h  gradient reduction + Adagrad (H6, H7)
 //   dev_hybrid.h   HybridHash bookkeeping kernels
 //   host_launch.h  device state of a plan, profiling brackets, launchers
@@ -59,6 +61,8 @@ namespace {
 #include "dev_small.h"
 #include "dev_rows.h"
 #include "dev_pool.h"
+#include "dev_mx.h"
+#include "dev_mx_lookup.h"
 #include "dev_adagrad.h"
 #include "dev_hybrid.h"
 #include "host_launch.h"
@@ -467,6 +471,43 @@ pk_status pk_backward_update(const pk_plan* plan, void* const* W, float* const* 
 {
     return backward_impl(plan, W, A, nullptr, grad_out, grad_row_stride, B, nnz, lr, eps, workspace, ws_bytes,
                          hip_stream);
+}
+
+// ---- pooled lookup from tables of microscaled 4-bit rows ---------------------------
+pk_status pk_mx_forward(const pk_plan* plan, const void* const* T, const int64_t* ids, const int32_t* offsets, int32_t B, int64_t nnz,
+                        float* out, int64_t out_row_stride, int32_t* error_word, void* hip_stream)
+{
+    try {
+        const char* who = "pk_mx_forward";
+        pk_status rc = check_batch(plan, B, nnz, who);
+        if (rc != PK_OK) return rc;
+        if (!T || !offsets || !out || !error_word || (!ids && nnz > 0)) return fail(PK_EINVAL, std::string(who) + ": NULL argument");
+        if (out_row_stride < plan->out_dim) return fail(PK_ESHAPE, std::string(who) + ": out_row_stride is smaller than out_dim");
+        const int P = (int)plan->packs.size();
+        for (int p = 0; p < P; ++p)
+            if (!T[p] || reinterpret_cast<uintptr_t>(T[p]) % 4) return fail(PK_EINVAL, std::string(who) + ": T[" + std::to_string(p) + "] is NULL or not 4-byte aligned");
+        DeviceState* ds = nullptr;
+        rc = ensure_device_state(plan, &ds);
+        if (rc != PK_OK) return rc;
+        hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+        MxJob job{};
+        for (int p = 0; p <= P; ++p) {
+            if (job.n_packs == kMxPacks || (p == P && job.n_packs)) {
+                job.B = B; job.n_fields = (int32_t)plan->fields.size(); job.nnz = nnz; job.fmeta = ds->fmeta; job.ids = ids; job.offsets = offsets;
+                job.out = out; job.out_stride = out_row_stride; job.error_word = error_word;
+                PK_LAUNCH("pk_mx_lookup", mx_lookup_kernel, dim3((unsigned)((job.n_items + NT - 1) / NT)), dim3(NT), 0, job);
+                job.n_packs = 0; job.n_items = 0;
+            }
+            if (p == P) break;
+            const Pack& k = plan->packs[p];
+            if (k.fields.empty()) continue;
+            const int chunks = (k.dim + 7) / 8;
+            job.pack[job.n_packs++] = MxPack{static_cast<const uint8_t*>(T[p]), ds->slot_field + k.first_slot, k.dim, chunks,
+                                             (int32_t)mx_row_bytes(PK_MXFP4, k.dim), (int32_t)mx_code_bytes(PK_MXFP4, k.dim), job.n_items};
+            job.n_items += (int64_t)k.fields.size() * B * chunks;
+        }
+        return PK_OK;
+    } catch (...) { return PK_ENOMEM; }
 }
 
 // ---- HybridHash ------------------------------------------------------------------

@@ -315,6 +315,10 @@ struct pk_plan {
 };
 
 namespace pk {
+// Microscaled rows: codes in whole 4-byte words, a scale byte per block of 32 columns, then up to a whole word.
+inline int64_t mx_code_bytes(int32_t format, int64_t cols) { return format == PK_MXFP4 ? (cols + 7) / 8 * 4 : (cols + 3) / 4 * 4; }
+inline int64_t mx_row_bytes(int32_t format, int64_t cols) { return (mx_code_bytes(format, cols) + (cols + 31) / 32 + 3) / 4 * 4; }
+
 void set_error(const std::string& msg);
 pk_status fail(pk_status s, const std::string& msg);
 // `room`: bytes that the workspace must fit, where the caller cannot give more (what is only kept to save time is left out)

@@ -154,12 +154,16 @@ class MicroBatchPipeline:
         self.ev_dedup[slot].record(self.side)
         return dict(slot=slot, B=B, nnz=nnz)
 
-    def pool(self, t: dict, out: torch.Tensor) -> torch.Tensor:
+    def pool(self, t: dict, out: torch.Tensor, keep: bool = False) -> torch.Tensor:
+        """keep: the pooled output is also kept in 8 bits, as t["kept"] (an ActivationCheckpoint), for the gradient of the
+        weights that multiply it; the micro-batches can then share one `out`."""
         layer = self.layer
         main = torch.cuda.current_stream(layer.device)
         main.wait_event(self.ev_dedup[t["slot"]])
         pk.pk_forward_pool(layer.plan, layer.W, t["B"], t["nnz"], out, out.stride(0), self.ws[t["slot"]],
                            self.ws_bytes, main.cuda_stream)
+        if keep:
+            t["kept"] = ActivationCheckpoint(t["B"], layer.out_dim, device=layer.device).quantize(out[:t["B"], :layer.out_dim])
         return out
 
     def backward_update(self, t: dict, grad_out: torch.Tensor, lr: float, eps: float) -> None:
@@ -170,6 +174,208 @@ class MicroBatchPipeline:
 
     def ctx_error(self, t: dict) -> int:
         return pk.pk_ctx_error(self.layer.plan, self.ws[t["slot"]])
+
+
+_MX_DTYPE = {torch.float32: pk.PK_F32, torch.bfloat16: pk.PK_BF16}
+
+
+def _device(device) -> torch.device:
+    device = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
+
+
+def _matrix(x: torch.Tensor, name: str, shape, device, dtypes=tuple(_MX_DTYPE)) -> int:
+    """Checks a matrix argument; returns its row stride in elements."""
+    if x.dim() != 2 or tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(x.shape)}")
+    if x.dtype not in dtypes:
+        raise ValueError(f"{name} must be one of {dtypes}, got {x.dtype}")
+    if x.device != device:
+        raise ValueError(f"{name} is on {x.device}, expected {device}")
+    if x.numel() == 0:
+        return x.shape[1]
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{name}: neighbouring columns must be neighbours in memory")
+    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+        raise ValueError(f"{name}: rows overlap")
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+class MxRows:
+    """A matrix as microscaled rows (4- or 8-bit elements, one scale per 32 columns) in one device buffer.
+
+        rows = MxRows(n_rows, cols, pk.PK_MXFP4).quantize(x)      # x: fp32 or bf16 [n_rows, cols]
+        y = rows.dequantize()                                     # fp32, or dtype=torch.bfloat16
+
+    `data`: a uint8 tensor [n_rows, stride] that holds (or will hold) the rows; else one is allocated whose rows are
+    `align` bytes apart or a multiple of that.  Buffer management only."""
+
+    def __init__(self, n_rows: int, cols: int, format: int, device: str = "cuda:0", data: torch.Tensor = None, align: int = 16):
+        self.n_rows, self.cols, self.format = int(n_rows), int(cols), int(format)
+        self.device = _device(device)
+        need = pk.pk_mx_row_bytes(self.format, self.cols)
+        if data is None:
+            stride = (need + align - 1) // align * align
+            data = torch.empty((self.n_rows, stride), dtype=torch.uint8, device=self.device)
+        stride = data.stride(0) if data.dim() == 2 and data.shape[0] > 1 else data.shape[-1]
+        if (data.dim() != 2 or data.dtype != torch.uint8 or data.shape[0] != self.n_rows or data.shape[1] < need or
+                data.device != self.device or (data.shape[1] > 1 and data.stride(1) != 1) or stride < need or stride % 4 or
+                data.data_ptr() % 4):
+            raise ValueError(f"data must be uint8 [{self.n_rows}, >= {need}] on {self.device}, rows a multiple of 4 bytes apart")
+        self.data, self.stride = data, stride
+
+    def quantize(self, x: torch.Tensor) -> "MxRows":
+        xs = _matrix(x, "x", (self.n_rows, self.cols), self.device)
+        with torch.cuda.device(self.device):
+            pk.pk_mx_quantize(x, _MX_DTYPE[x.dtype], xs, self.n_rows, self.cols, self.format, self.data, self.stride,
+                              torch.cuda.current_stream().cuda_stream)
+        return self
+
+    def dequantize(self, out: torch.Tensor = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        if out is None:
+            out = torch.empty((self.n_rows, self.cols), dtype=dtype, device=self.device)
+        os_ = _matrix(out, "out", (self.n_rows, self.cols), self.device)
+        with torch.cuda.device(self.device):
+            pk.pk_mx_dequantize(self.data, self.stride, self.n_rows, self.cols, self.format, out, _MX_DTYPE[out.dtype], os_,
+                                torch.cuda.current_stream().cuda_stream)
+        return out
+
+
+class ActivationCheckpoint(MxRows):
+    """The input of a dense layer (the pooled output, say) kept in 8 bits from the forward to the backward pass.
+
+        kept = ActivationCheckpoint(B, layer.out_dim).quantize(out)      # out's memory can be used again
+        ...
+        dw = kept.weight_grad(grad_y)                                    # [N, cols] = grad_y^T times the kept input
+        dw = kept.weight_grad(grad_y, out=dw, accumulate=True)           # a further micro-batch's share"""
+
+    def __init__(self, n_rows: int, cols: int, device: str = "cuda:0", data: torch.Tensor = None):
+        super().__init__(n_rows, cols, pk.PK_MXFP8, device=device, data=data)
+
+    def weight_grad(self, grad_y: torch.Tensor, out: torch.Tensor = None, accumulate: bool = False) -> torch.Tensor:
+        if grad_y.dim() != 2:
+            raise ValueError("grad_y must have two dimensions")
+        N = int(grad_y.shape[1])
+        gs = _matrix(grad_y, "grad_y", (self.n_rows, N), self.device)
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs out")
+            out = torch.empty((N, self.cols), dtype=torch.float32, device=self.device)
+        os_ = _matrix(out, "out", (N, self.cols), self.device, (torch.float32,))
+        with torch.cuda.device(self.device):
+            ws_bytes = pk.pk_mx_weight_grad_workspace_bytes(self.n_rows, N, self.cols)
+            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)       # (the allocator's: free again when the stream is past it)
+            pk.pk_mx_weight_grad(grad_y, _MX_DTYPE[grad_y.dtype], gs, self.data, self.stride, self.n_rows, N, self.cols, out, os_,
+                                 accumulate, ws, ws_bytes, torch.cuda.current_stream().cuda_stream)
+        return out
+
+
+class QuantizedLinear:
+    """A dense layer with its weights in 4 bits; its input is rounded to 4 bits on the way in.
+
+        dense = QuantizedLinear(weight, bias)            # weight: fp32 or bf16 [N, K]; bias: fp32 [N] or None
+        y = dense.forward(out)                           # out: fp32 or bf16 [M, K]; y: fp32, or dtype=torch.bfloat16
+
+    `weight` may be an MxRows of PK_MXFP4 rows instead.  Buffer management only."""
+
+    def __init__(self, weight, bias: torch.Tensor = None):
+        if not isinstance(weight, MxRows):
+            weight = MxRows(weight.shape[0], weight.shape[1], pk.PK_MXFP4, device=weight.device).quantize(weight)
+        if weight.format != pk.PK_MXFP4:
+            raise ValueError("weight rows must be PK_MXFP4")
+        self.weight, self.device = weight, weight.device
+        self.N, self.K = weight.n_rows, weight.cols
+        if bias is not None and (bias.dtype != torch.float32 or bias.shape != (self.N,) or bias.device != self.device or
+                                 (self.N > 1 and bias.stride(0) != 1)):
+            raise ValueError(f"bias must be fp32 [{self.N}], contiguous, on {self.device}")
+        self.bias = bias
+
+    def forward(self, x: torch.Tensor, out: torch.Tensor = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        if x.dim() != 2:
+            raise ValueError("x must have two dimensions")
+        M = int(x.shape[0])
+        xs = _matrix(x, "x", (M, self.K), self.device)
+        if out is None:
+            out = torch.empty((M, self.N), dtype=dtype, device=self.device)
+        os_ = _matrix(out, "out", (M, self.N), self.device)
+        with torch.cuda.device(self.device):
+            ws_bytes = pk.pk_mx_linear_workspace_bytes(M, self.N, self.K)
+            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+            pk.pk_mx_linear(x, _MX_DTYPE[x.dtype], xs, M, self.weight.data, self.weight.stride, self.N, self.K, self.bias, out,
+                            _MX_DTYPE[out.dtype], os_, ws, ws_bytes, torch.cuda.current_stream().cuda_stream)
+        return out
+
+
+class QuantizedEmbedding:
+    """The layer for serving: its tables in 4 bits (0.53 bytes a column from 32 columns on), pooled lookups only.
+
+        serve = QuantizedEmbedding.from_layer(layer)     # or QuantizedEmbedding(tables, fields) and load_table
+        out = serve.forward(ids, offsets, B)             # as PackedEmbedding.forward
+
+    `rows`: the packs' tables as microscaled rows where they are there already, uint8 [total_rows, pk_mx_row_bytes] each.
+    Buffer management only."""
+
+    def __init__(self, tables: Sequence[Tuple[int, int, int]], fields: Sequence[Tuple[int, int]], device: str = "cuda:0",
+                 rows: Sequence[torch.Tensor] = None, **plan_opts):
+        self.tables, self.fields = list(tables), list(fields)
+        self.device = _device(device)
+        self.plan = pk.pk_plan_create(self.tables, self.fields, **plan_opts)
+        self.n_packs = pk.pk_plan_num_packs(self.plan)
+        self.packs = [pk.pk_plan_pack_info(self.plan, p) for p in range(self.n_packs)]
+        self.table_slot = [pk.pk_plan_table_slot(self.plan, t) for t in range(len(self.tables))]
+        self.field_col = [pk.pk_plan_field_col(self.plan, f) for f in range(len(self.fields))]
+        self.out_dim = pk.pk_plan_out_dim(self.plan)
+        if rows is not None and len(rows) != self.n_packs:
+            raise ValueError(f"rows must be a list of {self.n_packs} packs")
+        # (rows stand close together: a lookup reads single rows, and what it reads is what it costs)
+        self.T = [MxRows(k["total_rows"], k["dim"], pk.PK_MXFP4, device=self.device, data=rows[p] if rows is not None else None, align=4)
+                  for p, k in enumerate(self.packs)]
+        for m in self.T:
+            if m.stride != pk.pk_mx_row_bytes(m.format, m.cols):
+                raise ValueError("a pack's rows must be pk_mx_row_bytes apart")
+        self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
+
+    @classmethod
+    def from_layer(cls, layer: PackedEmbedding, **plan_opts) -> "QuantizedEmbedding":
+        """The tables of a trained layer, rounded to 4 bits (plan_opts: as the layer's, where they change its packs)."""
+        if isinstance(layer, HybridEmbedding):
+            raise ValueError("rows in a Hot-storage are newer than the tables: quantize a PackedEmbedding")
+        q = cls(layer.tables, layer.fields, device=layer.device, **plan_opts)
+        if [(k["dim"], k["dtype"], k["total_rows"]) for k in q.packs] != [(k["dim"], k["dtype"], k["total_rows"]) for k in layer.packs]:
+            raise ValueError("the layer was made with other plan options")
+        for t in range(len(q.tables)):
+            q.load_table(t, layer.table_view(t))
+        return q
+
+    def close(self):
+        if self.plan:
+            pk.pk_plan_destroy(self.plan)
+            self.plan = None
+
+    def load_table(self, t: int, values: torch.Tensor) -> None:
+        """values: fp32 or bf16 [rows, dim]; rounded to 4 bits (a copy on the host is moved to the device first)."""
+        p, base = self.table_slot[t]
+        n, m = self.tables[t][0], self.T[p]
+        MxRows(n, m.cols, m.format, device=self.device, data=m.data[base:base + n]).quantize(values.to(self.device))
+
+    def forward(self, ids: torch.Tensor, offsets: torch.Tensor, B: int, out: torch.Tensor = None) -> torch.Tensor:
+        for x, name, dt, n in ((ids, "ids", torch.int64, None), (offsets, "offsets", torch.int32, len(self.fields) * B + 1)):
+            if x.dtype != dt or x.dim() != 1 or x.device != self.device or not x.is_contiguous() or (n is not None and x.shape[0] != n):
+                raise ValueError(f"{name} must be contiguous {dt} on {self.device}" + (f", {n} of them" if n is not None else ""))
+        if out is None:
+            out = torch.empty((B, self.out_dim), dtype=torch.float32, device=self.device)
+        stride = _matrix(out, "out", (B, self.out_dim), self.device, (torch.float32,))
+        with torch.cuda.device(self.device):
+            pk.pk_mx_forward(self.plan, [m.data for m in self.T], ids, offsets, B, int(ids.shape[0]), out, stride, self.error,
+                             torch.cuda.current_stream().cuda_stream)
+        return out
+
+    def error_word(self) -> int:
+        """Bit 0: some call's offsets were rejected since the word was last read (reading clears it; synchronises)."""
+        w = int(self.error.item())
+        if w:
+            self.error.zero_()
+        return w
 
 
 class HybridEmbedding(PackedEmbedding):

@@ -1,0 +1,194 @@
+"""The 4-bit dense product and the weight gradient from an 8-bit checkpoint, against the definition in 64 bits.
+
+Tolerance: the products of two elements and of their scales are exact in fp32 (linear: 2 x 2 digits; gradient: 24 x 4
+digits are added in three exact parts of 8 x 4); n of them are added in fp32 in some order, every addition off by at most
+2^-23 of what has been added so far (2^-24, twice that where the matrix unit truncates), three parts each for a gradient
+in fp32: n * 2^-23 * sum |terms| bounds it.  A result in bf16 is rounded once more: 2^-8 of it."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import mx
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def rand(shape, seed, spread=2.0):
+    rng = np.random.default_rng(seed)
+    return torch.from_numpy((rng.standard_normal(shape) * np.exp(rng.standard_normal((shape[0], 1)) * spread)).astype(np.float32))
+
+
+def quantized(x, fmt):
+    return mx.decode(mx.encode(x.float().numpy(), fmt), fmt, x.shape[1])
+
+
+def check_linear(M, N, K, xdt="f32", ydt="f32", bias=True, seed=0, x=None, pad=0):
+    from paper_2204_04903_amd.layer import QuantizedLinear
+    x = rand((M, K), seed).to(DT[xdt]) if x is None else x
+    w = rand((N, K), seed + 1, 0.5)
+    b = rand((N, 1), seed + 2)[:, 0].contiguous() if bias else None
+    dense = QuantizedLinear(w.cuda(), b.cuda() if bias else None)
+    out = torch.full((M, N + pad), float("nan"), dtype=DT[ydt], device="cuda")
+    dense.forward(x.cuda(), out=out[:, :N])
+    got = out.cpu().double().numpy()
+    assert np.isnan(got[:, N:]).all()
+    xq, wq = quantized(x, 0), quantized(w, 0)
+    ref, mag = xq @ wq.T, np.abs(xq) @ np.abs(wq).T
+    if bias:
+        ref, mag = ref + b.double().numpy(), mag + np.abs(b.double().numpy())
+    tol = (K + 1) * 2.0 ** -23 * mag + (2.0 ** -8 * np.abs(ref) if ydt == "bf16" else 0)
+    assert (np.abs(got[:, :N] - ref) <= tol * 1.01).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 16, 8), (1, 1000, 832), (2, 3, 31), (3, 64, 32), (4, 17, 33), (15, 65, 100), (16, 64, 128), (17, 130, 129),
+                                   (31, 64, 255), (32, 256, 256), (33, 100, 257), (64, 64, 1000), (65, 300, 511), (127, 129, 130), (128, 128, 512),
+                                   (129, 257, 640), (255, 63, 96), (300, 513, 832), (1000, 40, 64), (1, 5, 9000), (5, 260, 12000), (40, 70, 6007)])
+def test_linear_sizes(M, N, K):
+    check_linear(M, N, K, seed=M + N + K)
+
+
+@pytest.mark.parametrize("xdt", ["f32", "bf16"])
+@pytest.mark.parametrize("ydt", ["f32", "bf16"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("M", [1, 7, 50, 300])
+def test_linear_types(M, xdt, ydt, bias):
+    check_linear(M, 96, 200, xdt, ydt, bias, seed=M, pad=5)
+
+
+@pytest.mark.parametrize("M", [1, 9, 140])
+def test_linear_inputs_with_strides(M):
+    big = rand((M, 301), 5).cuda()
+    x = big[:, 1:288]
+    from paper_2204_04903_amd.layer import MxRows, QuantizedLinear
+    w = rand((70, 287), 6, 0.5)
+    for align in (4, 16, 64):                      # weight rows on 4-byte and on wider places
+        dense = QuantizedLinear(MxRows(70, 287, 0, align=align).quantize(w.cuda()))
+        y = dense.forward(x).cpu().double().numpy()
+        xq, wq = quantized(x.cpu(), 0), quantized(w, 0)
+        assert (np.abs(y - xq @ wq.T) <= 1.01 * 287 * 2.0 ** -23 * (np.abs(xq) @ np.abs(wq).T)).all()
+
+
+@pytest.mark.parametrize("M", [1, 20, 200])
+def test_linear_nan_and_infinities(M):
+    """a bad number spoils its row (of x) or its column (of the weights), no other"""
+    from paper_2204_04903_amd.layer import QuantizedLinear
+    x, w = rand((M, 300), 7).cuda(), rand((90, 300), 8).cuda()
+    clean = QuantizedLinear(w).forward(x)
+    x[M // 2, 299], w[33, 5] = float("inf"), float("nan")
+    y = QuantizedLinear(w).forward(x)
+    bad = torch.zeros_like(y, dtype=torch.bool)
+    bad[M // 2], bad[:, 33] = True, True
+    assert torch.equal(torch.isnan(y), bad)
+    assert torch.equal(y[~bad], clean[~bad])
+
+
+def test_linear_zero_rows_and_extreme_scales():
+    x = rand((40, 130), 9)
+    x[3] = 0
+    x[4] *= 2.0 ** 60
+    x[5] *= 2.0 ** -80
+    x[6, 32:64] = 0
+    check_linear(40, 33, 130, x=x, bias=False)
+
+
+def test_linear_no_rows():
+    from paper_2204_04903_amd.layer import QuantizedLinear
+    assert QuantizedLinear(rand((8, 40), 1).cuda()).forward(torch.empty(0, 40, device="cuda")).shape == (0, 8)
+
+
+def check_grad(B, N, K, dt="f32", seed=0, micro=1, pad=0, dy=None):
+    from paper_2204_04903_amd.layer import ActivationCheckpoint
+    x = rand((B, K), seed)
+    dy = rand((B, N), seed + 1).to(DT[dt]) if dy is None else dy
+    if B > 2:
+        x[1], dy[2] = 0, 0
+    out = torch.full((N, K + pad), float("nan"), device="cuda")
+    dw = out[:, :K]
+    step = (B + micro - 1) // micro if B else 1
+    for i, a in enumerate(range(0, max(B, 1), step)):
+        kept = ActivationCheckpoint(min(a + step, B) - a, K).quantize(x[a:a + step].cuda())
+        kept.weight_grad(dy[a:a + step].cuda(), out=dw, accumulate=i > 0)
+    got = out.cpu().double().numpy()
+    assert np.isnan(got[:, K:]).all()
+    xq, g = quantized(x, 1) if B else np.zeros((0, K)), dy.double().numpy()
+    ref, mag = g.T @ xq, np.abs(g).T @ np.abs(xq)
+    n = (3 if dt == "f32" else 1) * max(B, 1) + micro
+    assert (np.abs(got[:, :K] - ref) <= 1.01 * n * 2.0 ** -23 * mag).all()
+    return x, dy, got[:, :K]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("B,N,K", [(0, 5, 40), (1, 1, 1), (1, 8, 40), (2, 3, 31), (3, 17, 33), (7, 64, 64), (8, 128, 256), (15, 65, 100), (16, 16, 128), (31, 130, 129),
+                                   (32, 64, 255), (33, 128, 257), (63, 20, 96), (64, 256, 512), (65, 127, 31), (100, 300, 832), (257, 129, 130), (1000, 40, 70),
+                                   (513, 1, 1000), (129, 1000, 3), (5000, 33, 48), (2, 600, 6007)])
+def test_grad_sizes(B, N, K, dt):
+    check_grad(B, N, K, dt, seed=B + N + K, pad=B % 4)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("micro", [2, 3, 5])
+def test_grad_of_micro_batches(micro, dt):
+    check_grad(147, 70, 200, dt, seed=micro, micro=micro)
+
+
+def test_grad_fp32_is_not_cut_to_fewer_digits():
+    """one sample: every element is one product, exact but for the last rounding"""
+    from paper_2204_04903_amd.layer import ActivationCheckpoint
+    x, dy = rand((1, 64), 3), rand((1, 48), 4)
+    got = ActivationCheckpoint(1, 64).quantize(x.cuda()).weight_grad(dy.cuda()).cpu().double().numpy()
+    ref = dy.double().numpy().T @ quantized(x, 1)
+    # three exact parts are added: two roundings of 2^-23 at most
+    assert (np.abs(got - ref) <= 2.0 ** -22 * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_grad_against_differences(dt):
+    """L(W) = sum(dy * (X W^T)): its difference along single weights, in 64 bits, is the gradient's element"""
+    x, dy, got = check_grad(90, 20, 66, dt, seed=11)
+    xq, g = quantized(x, 1), dy.double().numpy()
+    W, h = np.random.default_rng(1).standard_normal((20, 66)), 2.0 ** -10
+    loss = lambda w: (g * (xq @ w.T)).sum()
+    mag = np.abs(g).T @ np.abs(xq)
+    for n, k in ((0, 0), (19, 65), (7, 31), (7, 32), (3, 64)):
+        up, down = W.copy(), W.copy()
+        up[n, k] += h
+        down[n, k] -= h
+        diff = (loss(up) - loss(down)) / (2 * h)
+        # 64-bit loss of about 2000 terms: 1e-13 of their magnitudes, over 2 h
+        noise = 1e-13 * (np.abs(g) * (np.abs(xq) @ np.abs(W).T)).sum() / h
+        assert abs(diff - got[n, k]) <= 3 * 91 * 2.0 ** -23 * mag[n, k] + noise
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_grad_strides_and_nan(dt):
+    from paper_2204_04903_amd.layer import ActivationCheckpoint, MxRows
+    B, N, K = 75, 50, 100
+    x, big = rand((B, K), 21), rand((B, N + 13), 22).to(DT[dt]).cuda()
+    dy = big[:, 3:3 + N]
+    ref = None
+    for data in (torch.empty((B, 108), dtype=torch.uint8, device="cuda"), torch.empty((B, 128), dtype=torch.uint8, device="cuda")):
+        kept = ActivationCheckpoint(B, K, data=data).quantize(x.cuda())
+        dw = kept.weight_grad(dy)
+        assert ref is None or torch.equal(dw, ref)           # the same sizes, the same order of sums
+        ref = dw
+    x[5, 40] = float("nan")
+    dw = ActivationCheckpoint(B, K).quantize(x.cuda()).weight_grad(dy)
+    bad = torch.zeros(N, K, dtype=torch.bool)
+    bad[:, 32:64] = True                                     # the block of the bad number, in every row
+    assert torch.equal(torch.isnan(dw).cpu(), bad)
+    assert torch.equal(dw.cpu()[~bad], ref.cpu()[~bad])
+    dy[6, 7] = float("inf")
+    dw = ActivationCheckpoint(B, K).quantize(rand((B, K), 21).cuda()).weight_grad(dy).cpu()
+    assert not torch.isfinite(dw[7]).any() and torch.isfinite(torch.cat([dw[:7], dw[8:]])).all()
+
+
+def test_grad_repeats_bit_for_bit():
+    from paper_2204_04903_amd.layer import ActivationCheckpoint
+    x, dy = rand((3000, 200), 31).cuda(), rand((3000, 100), 32).cuda()
+    kept = ActivationCheckpoint(3000, 200).quantize(x)
+    first = kept.weight_grad(dy)
+    for _ in range(3):
+        assert torch.equal(kept.weight_grad(dy), first)

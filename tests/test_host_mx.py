@@ -1,0 +1,150 @@
+"""Microscaled rows and what computes with them: sizes and refusals, without a GPU."""
+import pytest
+import torch
+
+from oracle import mx
+from paper_2204_04903_amd import binding as pk
+from paper_2204_04903_amd.layer import ActivationCheckpoint, MxRows, QuantizedLinear
+
+FAKE = 0x10000      # never dereferenced: every call below fails validation first
+
+
+def status(fn, *a, **kw):
+    with pytest.raises(pk.PkError) as e:
+        fn(*a, **kw)
+    return e.value.status
+
+
+def test_row_bytes():
+    for fmt in (0, 1):
+        for cols in list(range(1, 130)) + [832, 12000, 2 ** 31 - 1]:
+            assert pk.pk_mx_row_bytes(fmt, cols) == mx.row_bytes(fmt, cols)
+    for fmt, cols in ((2, 8), (-1, 8), (0, 0), (0, -4), (1, 2 ** 31)):
+        assert status(pk.pk_mx_row_bytes, fmt, cols) == pk.PK_EINVAL
+
+
+def quantize(**kw):
+    a = dict(src=FAKE, dt=0, stride=64, n=4, cols=64, fmt=0, rows=FAKE, rs=pk.pk_mx_row_bytes(0, 64))
+    a.update(kw)
+    return status(pk.pk_mx_quantize, a["src"], a["dt"], a["stride"], a["n"], a["cols"], a["fmt"], a["rows"], a["rs"])
+
+
+def dequantize(**kw):
+    a = dict(src=FAKE, dt=0, stride=64, n=4, cols=64, fmt=0, rows=FAKE, rs=pk.pk_mx_row_bytes(0, 64))
+    a.update(kw)
+    return status(pk.pk_mx_dequantize, a["rows"], a["rs"], a["n"], a["cols"], a["fmt"], a["src"], a["dt"], a["stride"])
+
+
+@pytest.mark.parametrize("call", [quantize, dequantize])
+def test_rounding_and_reading_back_refuse(call):
+    assert call(fmt=2) == pk.PK_EINVAL
+    assert call(dt=2) == pk.PK_EINVAL
+    assert call(src=None) == pk.PK_EINVAL
+    assert call(rows=None) == pk.PK_EINVAL
+    assert call(src=FAKE + 2) == pk.PK_EINVAL
+    assert call(src=FAKE + 1, dt=1) == pk.PK_EINVAL
+    assert call(rows=FAKE + 2) == pk.PK_EINVAL
+    assert call(rs=34) == pk.PK_EINVAL
+    assert call(rs=32) == pk.PK_EINVAL
+    assert call(stride=63) == pk.PK_EINVAL
+    assert call(n=-1) == pk.PK_ESHAPE
+    assert call(cols=0) == pk.PK_ESHAPE
+    assert call(n=2 ** 31) == pk.PK_EOVERFLOW
+    assert call(cols=2 ** 31) == pk.PK_EOVERFLOW
+
+
+def test_no_rows_is_no_work():
+    pk.pk_mx_quantize(None, 0, 0, 0, 64, 0, None, 0)
+    pk.pk_mx_dequantize(None, 0, 0, 64, 1, None, 1, 0)
+    pk.pk_mx_linear(None, 0, 0, 0, FAKE, 48, 4, 64, None, None, 0, 0, None, 0)
+
+
+def linear(**kw):
+    M, N, K = kw.pop("M", 4), kw.pop("N", 8), kw.pop("K", 64)
+    a = dict(x=FAKE, xdt=0, xs=K, w=FAKE, ws=48, bias=None, y=FAKE, ydt=0, ys=N, work=FAKE, nbytes=1 << 20)
+    a.update(kw)
+    return status(pk.pk_mx_linear, a["x"], a["xdt"], a["xs"], M, a["w"], a["ws"], N, K, a["bias"], a["y"], a["ydt"], a["ys"], a["work"], a["nbytes"])
+
+
+def test_linear_refuses():
+    for M, N, K in ((-1, 8, 64), (4, -8, 64), (4, 0, 64), (4, 8, 0)):
+        assert linear(M=M, N=N, K=K) == pk.PK_ESHAPE
+    for M, N, K in ((2 ** 31, 8, 64), (4, 2 ** 31, 64), (4, 8, 2 ** 31)):
+        assert linear(M=M, N=N, K=K) == pk.PK_EOVERFLOW
+    for bad in (dict(x=None), dict(y=None), dict(w=None), dict(work=None), dict(xdt=5), dict(ydt=-1), dict(xs=63), dict(ys=7), dict(ws=32),
+                dict(ws=50), dict(w=FAKE + 1), dict(bias=FAKE + 2), dict(x=FAKE + 1), dict(y=FAKE + 1)):
+        assert linear(**bad) == pk.PK_EINVAL, bad
+    assert linear(work=FAKE + 16) == pk.PK_EWORKSPACE
+    need = pk.pk_mx_linear_workspace_bytes(4, 8, 64)
+    assert linear(nbytes=need - 1) == pk.PK_EWORKSPACE
+    assert status(pk.pk_mx_linear_workspace_bytes, -1, 8, 64) == pk.PK_EINVAL
+    assert status(pk.pk_mx_linear_workspace_bytes, 4, 0, 64) == pk.PK_EINVAL
+
+
+def grad(**kw):
+    B, N, K = kw.pop("B", 4), kw.pop("N", 8), kw.pop("K", 64)
+    a = dict(dy=FAKE, dt=0, ds=N, x=FAKE, xs=pk.pk_mx_row_bytes(1, 64), dw=FAKE, dws=K, work=FAKE, nbytes=1 << 26)
+    a.update(kw)
+    return status(pk.pk_mx_weight_grad, a["dy"], a["dt"], a["ds"], a["x"], a["xs"], B, N, K, a["dw"], a["dws"], False, a["work"], a["nbytes"])
+
+
+def test_weight_grad_refuses():
+    for B, N, K in ((-1, 8, 64), (4, 0, 64), (4, -8, 64), (4, 8, 0)):
+        assert grad(B=B, N=N, K=K) == pk.PK_ESHAPE
+    for B, N, K in ((2 ** 31, 8, 64), (4, 2 ** 31, 64), (4, 8, 2 ** 31)):
+        assert grad(B=B, N=N, K=K) == pk.PK_EOVERFLOW
+    for bad in (dict(dy=None), dict(x=None), dict(dw=None), dict(work=None), dict(dt=3), dict(ds=7), dict(xs=64), dict(xs=70), dict(dws=63),
+                dict(dw=FAKE + 2), dict(dy=FAKE + 1), dict(x=FAKE + 2)):
+        assert grad(**bad) == pk.PK_EINVAL, bad
+    assert grad(work=FAKE + 128) == pk.PK_EWORKSPACE
+    assert grad(nbytes=pk.pk_mx_weight_grad_workspace_bytes(4, 8, 64) - 1) == pk.PK_EWORKSPACE
+    assert status(pk.pk_mx_weight_grad_workspace_bytes, 4, 8, 0) == pk.PK_EINVAL
+
+
+def test_lookup_refuses():
+    plan = pk.pk_plan_create([(100, 8, 0), (50, 16, 1)], [(0, 0), (1, 1)], max_batch=64, max_nnz=1000)
+    try:
+        def fwd(**kw):
+            a = dict(T=[FAKE, FAKE], ids=FAKE, offsets=FAKE, B=16, nnz=100, out=FAKE, stride=24, err=FAKE, plan=plan)
+            a.update(kw)
+            return status(pk.pk_mx_forward, a["plan"], a["T"], a["ids"], a["offsets"], a["B"], a["nnz"], a["out"], a["stride"], a["err"])
+        assert fwd(B=0) == fwd(B=65) == fwd(nnz=-1) == fwd(nnz=1001) == fwd(stride=23) == pk.PK_ESHAPE
+        for bad in (dict(T=[FAKE, None]), dict(T=[FAKE + 2, FAKE]), dict(ids=None), dict(offsets=None), dict(out=None), dict(err=None), dict(plan=None)):
+            assert fwd(**bad) == pk.PK_EINVAL, bad
+    finally:
+        pk.pk_plan_destroy(plan)
+
+
+def test_layer_refuses_matrices_that_do_not_fit():
+    # (on the CPU: every check stands before the first call of the library)
+    m = MxRows(6, 40, pk.PK_MXFP4, device="cpu")
+    assert m.stride == 32 and m.data.shape == (6, 32)
+    for x in (torch.zeros(6, 41), torch.zeros(5, 40), torch.zeros(6, 40, dtype=torch.float16), torch.zeros(40, 6).t(), torch.zeros(1, 40).expand(6, 40),
+              torch.zeros(240)):
+        with pytest.raises(ValueError):
+            m.quantize(x)
+        with pytest.raises(ValueError):
+            m.dequantize(out=x)
+    for data in (torch.zeros((6, 31), dtype=torch.uint8), torch.zeros((5, 32), dtype=torch.uint8), torch.zeros((6, 32)),
+                 torch.zeros((6, 23), dtype=torch.uint8), torch.zeros((6, 64), dtype=torch.uint8)[:, ::2], torch.zeros((6, 30), dtype=torch.uint8)):
+        with pytest.raises(ValueError):
+            MxRows(6, 40, pk.PK_MXFP4, device="cpu", data=data)
+    with pytest.raises(pk.PkError):
+        MxRows(6, 40, 3, device="cpu")
+    kept = ActivationCheckpoint(6, 40, device="cpu")
+    for g in (torch.zeros(5, 3), torch.zeros(6), torch.zeros(6, 3, dtype=torch.float64)):
+        with pytest.raises(ValueError):
+            kept.weight_grad(g)
+    with pytest.raises(ValueError):
+        kept.weight_grad(torch.zeros(6, 3), accumulate=True)
+    with pytest.raises(ValueError):
+        kept.weight_grad(torch.zeros(6, 3), out=torch.zeros(3, 40, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        QuantizedLinear(MxRows(6, 40, pk.PK_MXFP8, device="cpu"))
+    w = MxRows(6, 40, pk.PK_MXFP4, device="cpu")
+    for bias in (torch.zeros(5), torch.zeros(6, dtype=torch.bfloat16), torch.zeros(12)[::2]):
+        with pytest.raises(ValueError):
+            QuantizedLinear(w, bias)
+    for x in (torch.zeros(3, 41), torch.zeros(40), torch.zeros(3, 40, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            QuantizedLinear(w).forward(x)
