@@ -1,23 +1,193 @@
 // dW (+)= dY^T X, X an 8-bit checkpoint.
 // Part of pk_mx.hip: included there, in this order, inside its anonymous namespace.
 
-template <bool BF16>
-__global__ void __launch_bounds__(NT)
-mx_weight_grad_kernel(const char* __restrict__ dy, int64_t dy_stride, const uint8_t* __restrict__ xq, int64_t x_stride, int64_t B, int64_t K,
-                      int64_t items, float* __restrict__ dw, int64_t dw_stride, int accumulate)
+// ---------------------------------------------------------------------------
+// The sum runs over the samples, which are the rows of both operands, while a lane of a matrix instruction wants eight
+// consecutive samples of one column: a thread loads eight rows of four columns, and turns them over in registers on the way to
+// LDS.  X's elements become bf16 there (four digits and a power of two: exact); of an fp32 dY every element becomes three
+// bf16 numbers whose sum it is (8 + 8 + 8 digits, cut off, not rounded), so that all products are exact and what is
+// lost is what fp32 additions lose.
+// A block takes kGradN x kGradK elements of dW and a stretch of the samples, kGradB a step; the stretches' sums meet in a
+// second launch in their order, so that a result does not depend on which block came first.
+// ---------------------------------------------------------------------------
+constexpr int kGradN = 128, kGradK = 128, kGradB = 64;
+constexpr int kGradRow = kGradB * 2;             // bytes of a column's samples in LDS
+
+struct GradLayout { int64_t tiles_n, tiles_k, steps, splits, ld; size_t total; };
+inline GradLayout grad_layout(int64_t B, int64_t N, int64_t K)
 {
-    const int64_t words = (K + 3) / 4;
-    for (int64_t it = (int64_t)blockIdx.x * NT + threadIdx.x; it < items; it += (int64_t)gridDim.x * NT) {
-        const int64_t n = it / K, k = it - n * K;
-        float acc = 0.f;
-        for (int64_t b = 0; b < B; ++b) {
-            const char* d = dy + b * dy_stride;
-            const uint8_t* row = xq + b * x_stride;
-            const float g = BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t*>(d)[n]) : reinterpret_cast<const float*>(d)[n];
-            const f32x2v x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(row[k], mx_scale(row[words * 4 + k / 32]), false);
-            acc += g * x.x;
+    GradLayout L;
+    L.tiles_n = (N + kGradN - 1) / kGradN;
+    L.tiles_k = (K + kGradK - 1) / kGradK;
+    L.steps = (B + kGradB - 1) / kGradB;
+    const int64_t tiles = L.tiles_n * L.tiles_k;
+    L.splits = std::max<int64_t>(1, std::min<int64_t>(L.steps / 4, 512 / tiles));
+    L.ld = (K + 3) / 4 * 4;
+    L.total = L.splits > 1 ? (size_t)(L.splits * N * L.ld * 4) : kAlign;
+    return L;
+}
+
+// Where 16 bytes (samples 8 c .. 8 c + 7) of column r stand: neighbouring columns, which lanes read together, and every fourth,
+// which they write together, fall on different banks.
+__device__ __forceinline__ int grad_at(int r, int c) { return r * kGradRow + ((c ^ (r >> 2) ^ (r >> 1 & 1) << 2) & 7) * 16; }
+
+// eight samples of four columns, two to a word: turned over and stored
+__device__ __forceinline__ void grad_store(char* lds, int r, int c, const uint32_t (&u)[8][2])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+        uint4 v;
+        v.x = __builtin_amdgcn_perm(u[1][j >> 1], u[0][j >> 1], sel);
+        v.y = __builtin_amdgcn_perm(u[3][j >> 1], u[2][j >> 1], sel);
+        v.z = __builtin_amdgcn_perm(u[5][j >> 1], u[4][j >> 1], sel);
+        v.w = __builtin_amdgcn_perm(u[7][j >> 1], u[6][j >> 1], sel);
+        *reinterpret_cast<uint4*>(lds + grad_at(r + j, c)) = v;
+    }
+}
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+template <bool F32>
+__global__ void __launch_bounds__(256)
+mx_grad_kernel(const char* __restrict__ dy, int64_t dy_stride, const uint8_t* __restrict__ xq, int64_t x_stride, int64_t B, int N, int K,
+               int tiles_n, int tiles, int steps, int splits, float* __restrict__ out, int64_t out_stride, int64_t split_stride, int accumulate)
+{
+    constexpr int P = F32 ? 3 : 1;               // parts of an element of dY
+    __shared__ __attribute__((aligned(16))) char s_a[P * kGradN * kGradRow];
+    __shared__ __attribute__((aligned(16))) char s_b[kGradK * kGradRow];
+    // an XCD takes neighbouring pieces of the work: those of one stretch of samples share dY and X in its L2
+    const int n_work = tiles * splits, per = (n_work + 7) / 8, work = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || work >= n_work) return;
+    const int split = work / tiles, tile = work - split * tiles, tk = tile / tiles_n, tn = tile - tk * tiles_n;
+    const int step0 = (int)((int64_t)steps * split / splits), step1 = (int)((int64_t)steps * (split + 1) / splits);
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wn = wave & 1, wk = wave >> 1;
+    const int c4 = (t & 31) * 4, bg = t >> 5;    // this thread's columns and its eight samples of a step
+    const int n = tn * kGradN + c4, k = tk * kGradK + c4;
+    const int code_bytes = (K + 3) / 4 * 4, kw = min(k, code_bytes - 4);
+    // the scales of the tile's four blocks of columns: a whole word of the row (scales and zeros fill whole words)
+    const int scale_word = code_bytes + min(tk * (kGradK / 32), ((K + 31) / 32 - 1) & ~3), scale_shift = (c4 >> 5) * 8;
+    constexpr int E = F32 ? 4 : 2;
+    uint32_t a[8][F32 ? 4 : 2], x[8], s[8];
+    auto load = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t b = (int64_t)step * kGradB + bg * 8 + i;
+            const int64_t at = min(b, B - 1);
+            const char* d = dy + at * dy_stride + (int64_t)n * E;
+            if (n + 4 <= N) {
+                if constexpr (F32) load_u32<4>(reinterpret_cast<const uint32_t*>(d), a[i]);
+                else { const u32x2_any v = *reinterpret_cast<const u32x2_any*>(d); a[i][0] = v.x; a[i][1] = v.y; }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t v = 0;
+                    if (n + j < N) v = F32 ? reinterpret_cast<const uint32_t*>(d)[j] : reinterpret_cast<const uint16_t*>(d)[j];
+                    if constexpr (F32) a[i][j] = v;
+                    else a[i][j >> 1] = j & 1 ? a[i][j >> 1] | v << 16 : v;
+                }
+            }
+            const uint8_t* row = xq + at * x_stride;
+            x[i] = *reinterpret_cast<const uint32_t*>(row + kw);
+            s[i] = *reinterpret_cast<const uint32_t*>(row + scale_word);
+            if (b >= B) {                        // samples that are not there
+#pragma unroll
+                for (int j = 0; j < (F32 ? 4 : 2); ++j) a[i][j] = 0;
+                x[i] = 0; s[i] = 0;
+            }
         }
+    };
+    auto store = [&]() {
+        uint32_t u[8][2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float sc = mx_scale(s[i] >> scale_shift & 255u);
+            u[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], sc, false));
+            u[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], sc, true));
+        }
+        grad_store(s_b, c4, bg, u);
+        if constexpr (!F32) {
+            grad_store(s_a, c4, bg, a);
+        } else {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    u[i][0] = __builtin_amdgcn_perm(a[i][1], a[i][0], 0x07060302u);
+                    u[i][1] = __builtin_amdgcn_perm(a[i][3], a[i][2], 0x07060302u);
+#pragma unroll
+                    for (int j = 0; j < 4 && p < 2; ++j)
+                        a[i][j] = __float_as_uint(__uint_as_float(a[i][j]) - __uint_as_float(a[i][j] & 0xFFFF0000u));
+                }
+                grad_store(s_a + p * kGradN * kGradRow, c4, bg, u);
+            }
+        }
+    };
+    f32x16 acc[2][2] = {};
+    const int row_a = wn * 64 + (lane & 31), row_b = wk * 64 + (lane & 31);
+    if (step0 < step1) load(step0);
+    for (int step = step0; step < step1; ++step) {
+        store();
+        __syncthreads();
+        if (step + 1 < step1) load(step + 1);
+#pragma unroll
+        for (int kk = 0; kk < kGradB / 16; ++kk) {
+            const int c = kk * 2 + (lane >> 5);
+            bf16x8 fb[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) fb[j] = *reinterpret_cast<const bf16x8*>(s_b + grad_at(row_b, c) + j * 32 * kGradRow);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bf16x8 fa = *reinterpret_cast<const bf16x8*>(s_a + p * kGradN * kGradRow + grad_at(row_a, c) + i * 32 * kGradRow);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    float* o = out + split * split_stride;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int kc = tk * kGradK + wk * 64 + j * 32 + (lane & 31);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int nr = tn * kGradN + wn * 64 + i * 32 + (e >> 2) * 8 + (lane >> 5) * 4 + (e & 3);
+                if (nr < N && kc < K) {
+                    float* at = o + (int64_t)nr * out_stride + kc;
+                    *at = accumulate ? *at + acc[i][j][e] : acc[i][j][e];
+                }
+            }
+        }
+}
+
+// the stretches' sums, added up in their order
+__global__ void __launch_bounds__(NT)
+mx_grad_join_kernel(const float* __restrict__ part, int64_t ld, int64_t split_stride, int splits, int K, int64_t items, float* __restrict__ dw,
+                    int64_t dw_stride, int accumulate)
+{
+    const int64_t per_row = ld / 4;
+    for (int64_t it = (int64_t)blockIdx.x * NT + threadIdx.x; it < items; it += (int64_t)gridDim.x * NT) {
+        const int64_t n = it / per_row;
+        const int k = (int)(it - n * per_row) * 4;
+        const float* p = part + n * ld + k;
+        f32x4 v = *reinterpret_cast<const f32x4*>(p);
+        for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * split_stride);
         float* o = dw + n * dw_stride + k;
-        *o = accumulate ? *o + acc : acc;
+        const int m = K - k;
+        if (m >= 4) {
+            if (accumulate) v += *reinterpret_cast<const f32x4*>(o);
+            *reinterpret_cast<f32x4*>(o) = v;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (j < m) o[j] = accumulate ? o[j] + v[j] : v[j];
+        }
     }
 }

@@ -171,7 +171,7 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
 size_t pk_mx_weight_grad_workspace_bytes(int64_t B, int64_t N, int64_t K)
 {
     if (B < 0 || N <= 0 || K <= 0 || B > kMxMax || N > kMxMax || K > kMxMax) { set_error("pk_mx_weight_grad_workspace_bytes: bad sizes"); return 0; }
-    return kAlign;
+    return grad_layout(B, N, K).total;
 }
 
 pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_stride, const void* x_rows, int64_t x_row_stride,
@@ -191,10 +191,20 @@ pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_str
         if (misaligned(workspace, kAlign)) return fail(PK_EWORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
         if (ws_bytes < pk_mx_weight_grad_workspace_bytes(B, N, K)) return fail(PK_EWORKSPACE, std::string(who) + ": workspace is smaller than pk_mx_weight_grad_workspace_bytes");
         hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-        const int64_t items = N * K;
-        const auto kernel = dy_dtype == PK_BF16 ? mx_weight_grad_kernel<true> : mx_weight_grad_kernel<false>;
-        MX_LAUNCH("mx_weight_grad", kernel, dim3(mx_blocks_for(items)), dim3(NT), static_cast<const char*>(dy), dy_row_stride * (dy_dtype == PK_BF16 ? 2 : 4),
-                  static_cast<const uint8_t*>(x_rows), x_row_stride, B, K, items, dw, dw_row_stride, accumulate);
+        const GradLayout L = grad_layout(B, N, K);
+        const int64_t tiles = L.tiles_n * L.tiles_k;
+        if (tiles * L.splits > ((int64_t)1 << 30)) return fail(PK_EOVERFLOW, std::string(who) + ": N * K is too large");
+        const bool join = L.splits > 1;
+        const auto kernel = dy_dtype == PK_BF16 ? mx_grad_kernel<false> : mx_grad_kernel<true>;
+        MX_LAUNCH("mx_grad", kernel, dim3((unsigned)((tiles * L.splits + 7) / 8 * 8)), dim3(256), static_cast<const char*>(dy),
+                  dy_row_stride * (dy_dtype == PK_BF16 ? 2 : 4), static_cast<const uint8_t*>(x_rows), x_row_stride, B, (int)N, (int)K, (int)L.tiles_n,
+                  (int)tiles, (int)L.steps, (int)L.splits, join ? static_cast<float*>(workspace) : dw, join ? L.ld : dw_row_stride, N * L.ld,
+                  join ? 0 : accumulate);
+        if (join) {
+            const int64_t items = N * (L.ld / 4);
+            MX_LAUNCH("mx_grad_join", mx_grad_join_kernel, dim3(mx_blocks_for(items)), dim3(NT), static_cast<const float*>(workspace), L.ld, N * L.ld,
+                      (int)L.splits, (int)K, items, dw, dw_row_stride, accumulate);
+        }
         return PK_OK;
     });
 }
