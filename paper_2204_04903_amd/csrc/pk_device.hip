@@ -29,6 +29,7 @@
 #include <map>
 #include <mutex>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "pk_internal.h"
@@ -490,21 +491,28 @@ pk_status pk_mx_forward(const pk_plan* plan, const void* const* T, const int64_t
         rc = ensure_device_state(plan, &ds);
         if (rc != PK_OK) return rc;
         hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-        MxJob job{};
-        for (int p = 0; p <= P; ++p) {
-            if (job.n_packs == kMxPacks || (p == P && job.n_packs)) {
-                job.B = B; job.n_fields = (int32_t)plan->fields.size(); job.nnz = nnz; job.fmeta = ds->fmeta; job.ids = ids; job.offsets = offsets;
-                job.out = out; job.out_stride = out_row_stride; job.error_word = error_word;
-                PK_LAUNCH("pk_mx_lookup", mx_lookup_kernel, dim3((unsigned)((job.n_items + NT - 1) / NT)), dim3(NT), 0, job);
-                job.n_packs = 0; job.n_items = 0;
+        std::vector<int> order;                              // widest rows first: their work comes first in a launch
+        for (int p = 0; p < P; ++p)
+            if (!plan->packs[p].fields.empty()) order.push_back(p);
+        std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return plan->packs[x].dim > plan->packs[y].dim; });
+        for (size_t i = 0; i < order.size(); i += kMxPacks) {
+            MxJob job{};
+            int64_t items = 0;
+            for (size_t o = i; o < std::min(order.size(), i + kMxPacks); ++o) {
+                const Pack& k = plan->packs[order[o]];
+                int sh = 0;
+                while ((32 << sh) < k.dim) ++sh;
+                const int kind = sh == 0 ? (k.dim + 7) / 8 : k.dim % 32 == 0 && (k.dim / 32 & (k.dim / 32 - 1)) == 0 ? 5 : 6;
+                const int tiles = (B + (NT >> sh) - 1) / (NT >> sh);
+                job.pack[job.n_packs++] = MxPack{static_cast<const uint8_t*>(T[order[o]]), ds->slot_field + k.first_slot, k.dim, sh, kind,
+                                                 (int32_t)mx_row_bytes(PK_MXFP4, k.dim), (int32_t)mx_code_bytes(PK_MXFP4, k.dim),
+                                                 (int32_t)k.fields.size(), tiles, (int32_t)items};
+                items += (int64_t)k.fields.size() * tiles;
             }
-            if (p == P) break;
-            const Pack& k = plan->packs[p];
-            if (k.fields.empty()) continue;
-            const int chunks = (k.dim + 7) / 8;
-            job.pack[job.n_packs++] = MxPack{static_cast<const uint8_t*>(T[p]), ds->slot_field + k.first_slot, k.dim, chunks,
-                                             (int32_t)mx_row_bytes(PK_MXFP4, k.dim), (int32_t)mx_code_bytes(PK_MXFP4, k.dim), job.n_items};
-            job.n_items += (int64_t)k.fields.size() * B * chunks;
+            job.B = B; job.n_fields = (int32_t)plan->fields.size(); job.n_items = (int32_t)items; job.nnz = nnz;
+            job.seq_blocks = nnz >= (int64_t)kMxSeqAvg * B ? (int)std::min<int64_t>(1024, std::max<int64_t>(1, nnz / (kMxSeqAvg * (NT / 64)))) : 0;
+            job.fmeta = ds->fmeta; job.ids = ids; job.offsets = offsets; job.out = out; job.out_stride = out_row_stride; job.error_word = error_word;
+            PK_LAUNCH("pk_mx_lookup", mx_lookup_kernel, dim3((unsigned)(job.seq_blocks + items)), dim3(NT), 0, job);
         }
         return PK_OK;
     } catch (...) { return PK_ENOMEM; }
