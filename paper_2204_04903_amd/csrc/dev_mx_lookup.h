@@ -6,119 +6,124 @@
 // scales; Gather and SegmentReduction (Sec. II-D) of all packs in one launch, keys formed from the IDs as the pooling of
 // small batches does.
 //
-// A lane holds up to 32 columns of a row, one block, which is one wide access and, from 25 columns on, one for the scale; a
-// row of more columns is a group of 2, 4 or 8 lanes.  A block of the launch takes the bags of one field that its groups can
-// hold, one each, and deals them out by their number of rounds of R rows, longest first, so that the groups of a wavefront
-// have about as many (bags of 1 to 50 IDs in their own order: half of the lanes wait).  R rows and the next R IDs are in flight together;
-// a round's rows are added as a tree in fp32 (two digits each: exact unless the scales are far apart), the rounds in
-// double.  Fields of sequences (kMxSeqAvg IDs per bag on average and more) go to wavefronts of their own, which start first: there the groups of a
-// wavefront share a bag, and their sums meet by halves, every lane giving away half of its columns a step.
+// What a lookup costs is its requests: from an L2 246 G of them a second (row of 20 bytes, one access), and 135 G rows where codes and scale
+// are two accesses, because the second one finds the line not there yet either.  So a lane holds two words of codes, 16
+// columns, and the word behind them; the last lane of a row has the row's scales there and hands them to the others.
+// A wavefront, a block of its own, takes two bags per lane group, those with many rounds of R rows
+// together with those with few.  A round's IDs are read by all lanes, R of them next to one another per bag, each ID once; its keys
+// go through LDS; its rows are in flight together with the next round's IDs.  A round's rows are added as a tree in fp32 (two digits each: exact unless the
+// scales are far apart), the rounds in double.  Fields of sequences (kMxSeqAvg IDs per bag on average and more) go to
+// wavefronts of their own, which start first: there the groups of a wavefront share a bag, and their sums meet by halves, every
+// lane giving away half of its columns a step.
 // ---------------------------------------------------------------------------
 constexpr int kMxPacks = 16;     // packs of one launch
-constexpr int kMxRound = 8;
 constexpr int kMxSeqAvg = 64;
+constexpr int64_t kMxSeqBlocks = 4096, kMxSeqIds = 512;      // wavefronts for their bags, at most, and IDs that there should be for each
+constexpr int kMxXcdFields = 32; // fields from which every one has its XCD
 constexpr int kMxBins = 32;      // numbers of rounds that are told apart
 struct MxPack {
     const uint8_t* T; const int32_t* slot_field;
-    int32_t D, sh, kind, stride, code_bytes;     // dimension; log2 of the lanes per row; 1 to 4: words of a row of one lane, 5: whole blocks, 6: others
-    int32_t n_fields, tiles, item_begin;         // fields; blocks per field; first block of the pack among the launch's
+    int32_t D, kind, stride, code_bytes;         // dimension; MxKind; bytes of a row and of its codes
+    int32_t n_fields, tiles, item_begin, turn, p;   // fields; blocks per field; first block of the pack among the launch's; its first field's XCD; pack
 };
 struct MxJob {
     MxPack pack[kMxPacks];
-    int32_t n_packs, B, n_fields, n_items, seq_blocks; int64_t nnz;
+    int32_t n_packs, B, n_fields, by_xcd, seq_blocks; int64_t nnz;
     const FieldMeta* fmeta; const int64_t* ids; const int32_t* offsets;
     float* out; int64_t out_stride; int32_t* error_word;
 };
 
-// what a lane holds of a row: W words of codes and the scale
-template <int W, bool MULTI, bool RAGGED>
-struct MxPiece {
-    uint32_t w[W], s;
-    __device__ __forceinline__ void load(const uint8_t* row, int li, int code_bytes)
-    {
-        const uint32_t* at = reinterpret_cast<const uint32_t*>(row);
-        if constexpr (RAGGED) {
-            const int words = code_bytes >> 2, blk = min(li, (words - 1) >> 2);
-#pragma unroll
-            for (int j = 0; j < W; ++j) w[j] = at[min(4 * blk + j, words - 1)];
-            s = row[code_bytes + blk];
-        } else if constexpr (MULTI) {
-            load_u32<4>(at + 4 * li, w);
-            s = row[code_bytes + li];
-        } else if constexpr (W == 1) {
-            uint32_t v[2];
-            load_u32<2>(at, v);
-            w[0] = v[0]; s = v[1];
-        } else if constexpr (W == 2) {
-            typedef uint32_t u32x3 __attribute__((ext_vector_type(3), aligned(4)));
-            const u32x3 v = *reinterpret_cast<const u32x3*>(at);
-            w[0] = v.x; w[1] = v.y; s = v.z;
-        } else if constexpr (W == 3) {
-            uint32_t v[4];
-            load_u32<4>(at, v);
-            w[0] = v[0]; w[1] = v[1]; w[2] = v[2]; s = v[3];
-        } else {
-            load_u32<4>(at, w);
-            s = at[4];
-        }
-    }
-};
+// Kinds of rows: 0: up to 8 columns, one lane with the row's one word and its scale; k: up to 2^(k + 3) columns, 2^(k - 1)
+// lanes of two words each, the last ones ending with the row; 5: more than 128 columns, 16 lanes, scales in more than one word.
+constexpr int kMxKinds = 6;
+constexpr int mx_lanes_shift(int kind) { return kind == 0 ? 0 : kind - 1; }
+inline int mx_kind(int dim) { int k = 0; while ((8 << k) < dim) ++k; return k; }
 
-struct MxField {
-    const uint8_t* T; const int64_t* ids; int64_t nnz;
+struct MxSrc {
+    const uint8_t* T; const int64_t* ids;
     uint32_t base, rows, stride; uint64_t magic;
     int code_bytes;
-    __device__ __forceinline__ MxField(const MxJob& job, const MxPack& k, const FieldMeta& m)
-        : T(as_global(k.T)), ids(as_global(job.ids)), nnz(job.nnz), base(m.base_row), rows(m.rows), stride((uint32_t)k.stride), magic(m.magic),
-          code_bytes(k.code_bytes) {}
-    // R IDs from q on, those from e (> q) on replaced by the last one before it
-    template <int R>
-    __device__ __forceinline__ void load_ids(int q, int e, int64_t (&id)[R]) const
+    __device__ __forceinline__ MxSrc(const MxJob& job, const MxPack& k, const FieldMeta& m)
+        : T(as_global(k.T)), ids(as_global(job.ids)), base(m.base_row), rows(m.rows), stride((uint32_t)k.stride), magic(m.magic), code_bytes(k.code_bytes) {}
+    __device__ __forceinline__ uint32_t key(int64_t id) const { return base + fold_id(id, rows, magic); }
+};
+
+template <int KIND>
+struct MxLane {
+    static constexpr int W = KIND == 0 ? 1 : 2, SH = mx_lanes_shift(KIND), L = 1 << SH, G = 64 >> SH;
+    int c, sh0, sh1;                                       // first word; where the words' scales are in the scale word
+    __device__ __forceinline__ explicit MxLane(int code_bytes)
     {
-#pragma unroll
-        for (int i = 0; i < R; ++i) id[i] = ids[min(q + i, e - 1)];
+        c = KIND == 0 ? 0 : min(2 * (int)(threadIdx.x & (L - 1)), (code_bytes >> 2) - 2);
+        sh0 = (c >> 2) * 8; sh1 = ((c + 1) >> 2) * 8;
     }
-    template <int W, bool MULTI, bool RAGGED, int R>
-    __device__ __forceinline__ void add_rows(const int64_t (&id)[R], int left, int li, double (&acc)[8 * W]) const
+    // the rows of R keys in LDS, of which `left` count
+    template <int R>
+    __device__ __forceinline__ void add_rows(const MxSrc& src, const uint32_t* s_key, int left, double (&acc)[8 * W]) const
     {
-        MxPiece<W, MULTI, RAGGED> v[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) v[i].load(T + (size_t)(base + fold_id(id[i], rows, magic)) * stride, li, code_bytes);
-        float sc[R];
+        uint32_t w[R][W], s[R], s2[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            sc[i] = mx_scale(v[i].s & 255u);
-            if (i > 0 && i >= left) {                      // past the bag's end: nothing
-                sc[i] = 0.f;
-#pragma unroll
-                for (int j = 0; j < W; ++j) v[i].w[j] = 0;
+            const uint8_t* row = src.T + (size_t)s_key[i] * src.stride;
+            const uint32_t* at = reinterpret_cast<const uint32_t*>(row) + c;
+            if constexpr (W == 1) {
+                uint32_t v[2];
+                load_u32<2>(at, v);
+                w[i][0] = v[0]; s[i] = v[1];
+            } else if constexpr (KIND == 5) {
+                uint32_t v[2];
+                load_u32<2>(at, v);
+                w[i][0] = v[0]; w[i][1] = v[1];
+                s[i] = row[src.code_bytes + (c >> 2)]; s2[i] = row[src.code_bytes + ((c + 1) >> 2)];
+            } else {
+                typedef uint32_t u32x3 __attribute__((ext_vector_type(3), aligned(4)));
+                const u32x3 v = *reinterpret_cast<const u32x3*>(at);
+                w[i][0] = v.x; w[i][1] = v.y; s[i] = v.z;
             }
+        }
+        float f0[R], f1[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if constexpr (KIND == 2) s[i] = (uint32_t)__builtin_amdgcn_mov_dpp((int)s[i], 0xF5, 0xF, 0xF, true);        // lanes 1 1 3 3
+            if constexpr (KIND == 3) s[i] = (uint32_t)__builtin_amdgcn_mov_dpp((int)s[i], 0xFF, 0xF, 0xF, true);        // lane 3
+            if constexpr (KIND == 4) s[i] = (uint32_t)__shfl((int)s[i], threadIdx.x | 7, 64);
+            f0[i] = mx_scale((KIND == 5 ? s[i] : KIND <= 1 ? s[i] : s[i] >> sh0) & 255u);
+            f1[i] = mx_scale((KIND == 5 ? s2[i] : KIND <= 1 ? s[i] : s[i] >> sh1) & 255u);
+            if (i > 0)                                     // past the bag's end: nothing (its last row again, whose scale does no harm)
+#pragma unroll
+                for (int j = 0; j < W; ++j) w[i][j] = i < left ? w[i][j] : 0;
         }
 #pragma unroll
         for (int j = 0; j < W; ++j)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int h = 0; h < 4; ++h) {
                 f32x2v x[R];
 #pragma unroll
-                for (int i = 0; i < R; ++i)
-                    x[i] = c == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v[i].w[j], sc[i], 0)
-                         : c == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v[i].w[j], sc[i], 1)
-                         : c == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v[i].w[j], sc[i], 2)
-                                  : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v[i].w[j], sc[i], 3);
+                for (int i = 0; i < R; ++i) {
+                    const float f = j ? f1[i] : f0[i];
+                    x[i] = h == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i][j], f, 0)
+                         : h == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i][j], f, 1)
+                         : h == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i][j], f, 2)
+                                  : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i][j], f, 3);
+                }
 #pragma unroll
                 for (int d = 1; d < R; d *= 2)
 #pragma unroll
                     for (int i = 0; i + d < R; i += 2 * d) { x[i].x += x[i + d].x; x[i].y += x[i + d].y; }
-                acc[8 * j + 2 * c] += (double)x[0].x;
-                acc[8 * j + 2 * c + 1] += (double)x[0].y;
+                acc[8 * j + 2 * h] += (double)x[0].x;
+                acc[8 * j + 2 * h + 1] += (double)x[0].y;
             }
     }
 };
 
-__device__ __forceinline__ bool mx_is_seq(const MxJob& job, int f)
+__device__ __forceinline__ void mx_wave_order()
 {
-    const int32_t* o = as_global(job.offsets) + (int64_t)f * job.B;
-    return job.seq_blocks && (int64_t)o[job.B] - o[0] >= (int64_t)kMxSeqAvg * job.B;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+__device__ __forceinline__ bool mx_is_seq(const MxJob& job, int64_t field_ids)
+{
+    return job.seq_blocks && field_ids >= (int64_t)kMxSeqAvg * job.B;
 }
 // bag b of a field: its positions, none and the error raised where its offsets are no range of the IDs
 __device__ __forceinline__ void mx_bag(const MxJob& job, const int32_t* offs, int b, bool report, int& q, int& e)
@@ -130,59 +135,116 @@ __device__ __forceinline__ void mx_bag(const MxJob& job, const int32_t* offs, in
     }
 }
 
-// a block's tile of a field: s_bin [kMxBins], s_bag [256]
-template <int W, bool MULTI, bool RAGGED>
-__device__ __forceinline__ void mx_tile(const MxJob& job, const MxPack& k, const FieldMeta& m, const int32_t* offs, int tile, int* s_bin, int* s_bag)
+// A wavefront's tile of a field.  s_bin [kMxBins], s_bag [128], s_key [2][64 * 8], s_out [128 * 16]
+template <int KIND, int R>
+__device__ __forceinline__ void mx_tile(const MxJob& job, const MxPack& k, const FieldMeta& m, const int32_t* offs, int tile, int* s_bin, int* s_bag,
+                                        uint32_t (*s_key)[512], float* s_out)
 {
-    constexpr int R = kMxRound;
-    const int t = threadIdx.x, sh = MULTI ? k.sh : 0, n_groups = NT >> sh, b0 = tile * n_groups, nb = min(n_groups, job.B - b0);
-    const MxField src(job, k, m);
-    {
-        if (t < kMxBins) s_bin[t] = 0;
-        __syncthreads();
-        int pos = 0, bin = 0;
-        if (t < nb) {
-            int q, e;
-            mx_bag(job, offs, b0 + t, true, q, e);
-            bin = kMxBins - 1 - min((e - q + R - 1) / R, kMxBins - 1);
-            pos = atomicAdd(&s_bin[bin], 1);
-        }
-        __syncthreads();
-        if (t < 64) {                                      // bins to places (the first wavefront, half of it idle)
-            int v = t < kMxBins ? s_bin[t] : 0;
-            const int own = v;
+    using Lane = MxLane<KIND>;
+    constexpr int G = Lane::G, W = Lane::W, SH = Lane::SH, COLS = 8 * W * Lane::L;
+    constexpr bool STAGED = R > 1;                         // (sums go out together; one-hot bags as they are done)
+    const int lane = threadIdx.x, b0 = tile * 2 * G, nb = min(2 * G, job.B - b0);
+    const MxSrc src(job, k, m);
+    // the bags by their number of rounds, most first
+    if (R > 1) {
+        if (lane < kMxBins) s_bin[lane] = 0;
+        mx_wave_order();
+        int bin[2] = {0, 0}, pos[2] = {0, 0};
 #pragma unroll
-            for (int o = 1; o < kMxBins; o <<= 1) { const int u = __shfl_up(v, o, 64); if (t >= o) v += u; }
-            if (t < kMxBins) s_bin[t] = v - own;
+        for (int h = 0; h < 2; ++h) {
+            const int i = lane + 64 * h;
+            if (i < nb) {
+                int q, e;
+                mx_bag(job, offs, b0 + i, true, q, e);
+                bin[h] = kMxBins - 1 - min((int)((unsigned)(e - q + R - 1) / R), kMxBins - 1);
+                pos[h] = atomicAdd(&s_bin[bin[h]], 1);
+            }
         }
-        __syncthreads();
-        if (t < nb) s_bag[s_bin[bin] + pos] = b0 + t;
-        __syncthreads();
+        mx_wave_order();
+        int v = lane < kMxBins ? s_bin[lane] : 0;
+        const int own = v;
+#pragma unroll
+        for (int o = 1; o < kMxBins; o <<= 1) { const int u = __shfl_up(v, o, 64); if (lane >= o) v += u; }
+        mx_wave_order();
+        if (lane < kMxBins) s_bin[lane] = v - own;
+        mx_wave_order();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (lane + 64 * h < nb) s_bag[s_bin[bin[h]] + pos[h]] = b0 + lane + 64 * h;
+        mx_wave_order();
     }
-    const int g = t >> sh, li = t & ((1 << sh) - 1);
-    if (g >= nb) return;
-    const int b = s_bag[g];
-    int q, e;
-    mx_bag(job, offs, b, false, q, e);
-    const int len = e - q;
+    const int g = lane >> SH, i1 = min(g, nb - 1), i2 = min(2 * G - 1 - g, nb - 1);
+    int bag = R > 1 ? s_bag[i1] : b0 + i1, bag2 = R > 1 ? s_bag[i2] : b0 + i2;
+    int q, e, q2, e2;
+    mx_bag(job, offs, bag, R == 1 && g < nb, q, e);
+    mx_bag(job, offs, bag2, R == 1 && 2 * G - 1 - g < nb, q2, e2);
+    int todo = (g < nb) + (g < nb && 2 * G - 1 - g < nb);  // bags that this group has left to write
+    if (todo == 0) q = e = 0;
+    const Lane me(src.code_bytes);
+    int q0 = q;                                            // where the bag begins
     double acc[8 * W] = {};
-    int64_t id[R], next[R];
-    if (q < e) src.template load_ids<R>(q, e, id);
-    while (q < e) {
-        src.template load_ids<R>(min(q + R, e - 1), e, next);
-        src.template add_rows<W, MULTI, RAGGED, R>(id, e - q, li, acc);
+    // the IDs of a round: lane l reads number l % R of groups l / R, l / R + 64 / R ...
+    constexpr int N = G * R <= 64 ? 1 : G * R / 64;
+    int64_t id[N];
+    auto ask = [&](int at, int end) {                      // (a group's first position and its bag's end)
 #pragma unroll
-        for (int i = 0; i < R; ++i) id[i] = next[i];
-        q += R;
+        for (int n = 0; n < N; ++n) {
+            const int from = ((lane + 64 * n) / R) << SH, p = __shfl(at, from, 64), z = __shfl(end, from, 64);
+            id[n] = 0;
+            if (lane + 64 * n < G * R && p < z) id[n] = src.ids[min(p + lane % R, z - 1)];
+        }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) s_key[buf][lane + 64 * n] = src.key(id[n]);
+        mx_wave_order();
+    };
+    auto write = [&]() {
+        const double scale = m.pool == PK_MEAN && e > q0 ? 1.0 / (double)(e - q0) : 1.0;
+        float* o = STAGED ? s_out + (bag - b0) * COLS + 8 * me.c : as_global(job.out) + (size_t)bag * (size_t)job.out_stride + m.col + 8 * me.c;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { y[i] = (float)(acc[8 * j + i] * scale); acc[8 * j + i] = 0.0; }
+            store_f8<false>(reinterpret_cast<char*>(o + 8 * j), STAGED ? 8 : k.D - 8 * (me.c + j), y);
+        }
+        --todo;
+        bag = bag2;
+        q = q0 = todo ? q2 : 0;
+        e = todo ? e2 : 0;
+    };
+    ask(q, e);
+    put(0);
+    for (int buf = 0; __any(todo > 0); buf ^= 1) {
+        // (a bag without positions still takes a round, of which nothing counts: it is written after it)
+        const bool ends = q + R >= e;
+        const int nq = ends ? (todo > 1 ? q2 : 0) : q + R, ne = ends ? (todo > 1 ? e2 : 0) : e;
+        ask(nq, ne);
+        if (q < e) me.template add_rows<R>(src, s_key[buf] + g * R, e - q, acc);
+        put(buf ^ 1);
+        if (todo > 0) {
+            if (ends) write();
+            else q += R;
+        }
     }
-    const double scale = m.pool == PK_MEAN && len > 0 ? 1.0 / (double)len : 1.0;
-    float* o = as_global(job.out) + (size_t)b * (size_t)job.out_stride + m.col + 32 * li;
+    if (!STAGED) return;
+    mx_wave_order();
+    // rows of the output in whole, 16 bytes a lane
+    constexpr int PER = COLS / 4;
+    const int col = 4 * (lane % PER), left = k.D - col;
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = (float)(acc[8 * j + i] * scale);
-        store_f8<false>(reinterpret_cast<char*>(o + 8 * j), k.D - 32 * li - 8 * j, y);
+    for (int r = lane / PER; r < 2 * G; r += 64 / PER) {
+        if (r >= nb || left <= 0) continue;
+        const f32x4 y = *reinterpret_cast<const f32x4*>(s_out + r * COLS + col);
+        float* o = as_global(job.out) + (size_t)(b0 + r) * (size_t)job.out_stride + m.col + col;
+        if (left >= 4) {
+            *reinterpret_cast<f32x4*>(o) = y;
+        } else {
+            o[0] = y.x;
+            if (left > 1) o[1] = y.y;
+            if (left > 2) o[2] = y.z;
+        }
     }
 }
 
@@ -201,36 +263,41 @@ __device__ __forceinline__ void mx_halve(double* acc, int o, bool upper)
     }
 }
 
-template <int W, bool MULTI, bool RAGGED>
-__device__ __forceinline__ void mx_seq_bag(const MxJob& job, const MxPack& k, const FieldMeta& m, const int32_t* offs, int b)
+template <int KIND>
+__device__ __forceinline__ void mx_seq_bag(const MxJob& job, const MxPack& k, const FieldMeta& m, const int32_t* offs, int b, uint32_t (*s_key)[512])
 {
-    constexpr int R = kMxRound;
-    const int lane = threadIdx.x & 63, sh = MULTI ? k.sh : 0, g = lane >> sh, li = lane & ((1 << sh) - 1), n_groups = 64 >> sh;
-    const MxField src(job, k, m);
+    using Lane = MxLane<KIND>;
+    constexpr int R = 8, G = Lane::G, W = Lane::W, SH = Lane::SH, C = 8 * W, N = G * R / 64 > 0 ? G * R / 64 : 1;
+    const int lane = threadIdx.x, g = lane >> SH;
+    const MxSrc src(job, k, m);
     int q0, e;
     mx_bag(job, offs, b, lane == 0, q0, e);
-    double acc[8 * W] = {};
-    int64_t id[R], next[R];
-    int q = q0 + g * R;
-    if (q < e) src.template load_ids<R>(q, e, id);
-    while (q < e) {
-        src.template load_ids<R>(min(q + R * n_groups, e - 1), e, next);
-        src.template add_rows<W, MULTI, RAGGED, R>(id, e - q, li, acc);
+    const Lane me(src.code_bytes);
+    double acc[C] = {};
+    int64_t id[N];
+    auto ask = [&](int at) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) id[i] = next[i];
-        q += R * n_groups;
+        for (int n = 0; n < N; ++n)
+            if (lane + 64 * n < G * R) id[n] = src.ids[min(at + lane + 64 * n, e - 1)];
+    };
+    int buf = 0;
+    if (q0 < e) ask(q0);
+    for (int q = q0; q < e; q += G * R) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (lane + 64 * n < G * R) s_key[buf][lane + 64 * n] = src.key(id[n]);
+        mx_wave_order();
+        if (q + G * R < e) ask(q + G * R);
+        if (q + g * R < e) me.template add_rows<R>(src, s_key[buf] + g * R, e - q - g * R, acc);
+        buf ^= 1;
     }
-    // six steps less the row's lanes; W == 3 has no halves: its last word is zeros
-    constexpr int C = W == 3 ? 32 : 8 * W;
-    double a[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i) a[i] = i < 8 * W ? acc[i] : 0.0;
-    int col = 0, n = C, o = 1 << sh;
-    auto step = [&](auto N) {
+    int col = 0, n = C, o = 1 << SH;
+    auto step = [&](auto H) {
+        constexpr int have = decltype(H)::value;
         if (o < 64) {
             const bool upper = (lane & o) != 0;
-            mx_halve<decltype(N)::value>(a, o, upper);
-            if constexpr (decltype(N)::value > 1) { n /= 2; col += upper ? n : 0; }
+            mx_halve<have>(acc, o, upper);
+            if constexpr (have > 1) { n /= 2; col += upper ? n : 0; }
             o *= 2;
         }
     };
@@ -238,47 +305,59 @@ __device__ __forceinline__ void mx_seq_bag(const MxJob& job, const MxPack& k, co
     step(std::integral_constant<int, C / 2>{});
     step(std::integral_constant<int, C / 4>{});
     step(std::integral_constant<int, (C >= 16 ? C / 8 : 1)>{});
-    step(std::integral_constant<int, (C >= 32 ? C / 16 : 1)>{});
     step(std::integral_constant<int, 1>{});
-    // n columns are left in a lane: from col on of the row's lane li (several lanes may hold the same ones)
+    step(std::integral_constant<int, 1>{});
+    // n columns are left in a lane: from col on of its 16 (several lanes may hold the same ones)
     const double scale = m.pool == PK_MEAN && e > q0 ? 1.0 / (double)(e - q0) : 1.0;
     float* out = as_global(job.out) + (size_t)b * (size_t)job.out_stride + m.col;
+    col += 8 * me.c;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n && 32 * li + col + i < k.D) out[32 * li + col + i] = (float)(a[i] * scale);
+    for (int i = 0; i < 4; ++i)
+        if (i < n && col + i < k.D) out[col + i] = (float)(acc[i] * scale);
 }
 
-#define MX_KINDS(call)                                              \
-    switch (k.kind) {                                               \
-        case 1: call(1, false, false); break;                       \
-        case 2: call(2, false, false); break;                       \
-        case 3: call(3, false, false); break;                       \
-        case 4: call(4, false, false); break;                       \
-        case 5: call(4, true, false); break;                        \
-        default: call(4, true, true); break;                        \
+#define MX_KINDS(call)                     \
+    switch (k.kind) {                      \
+        case 0: call(0); break;            \
+        case 1: call(1); break;            \
+        case 2: call(2); break;            \
+        case 3: call(3); break;            \
+        case 4: call(4); break;            \
+        default: call(5); break;           \
     }
 
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(64)
 mx_lookup_kernel(MxJob job)
 {
-    __shared__ int s_bin[kMxBins], s_bag[NT];
-    const int item = (int)blockIdx.x - job.seq_blocks;
+    __shared__ int s_bin[kMxBins], s_bag[128];
+    __shared__ __attribute__((aligned(16))) uint32_t s_key[2][512];
+    __shared__ __attribute__((aligned(16))) float s_out[128 * 16];     // a tile's sums
+    const int item = (int)blockIdx.x - job.seq_blocks, lane = threadIdx.x;
+    const int32_t* offsets = as_global(job.offsets);
     if (item < 0) {
-        // the bags of all sequence fields, one after the other, dealt to the wavefronts
-        const int lane = threadIdx.x & 63, n_waves = job.seq_blocks * (NT / 64);
-        int64_t base = 0, next = (int)blockIdx.x * (NT / 64) + (threadIdx.x >> 6);
-        for (int p = 0; p < job.n_packs; ++p) {
-            const MxPack& k = job.pack[p];
-            for (int j0 = 0; j0 < k.n_fields; j0 += 64) {
-                bool seq = false;
-                if (j0 + lane < k.n_fields) seq = mx_is_seq(job, as_global(k.slot_field)[j0 + lane]);
-                for (uint64_t todo = __ballot(seq); todo; todo &= todo - 1) {
-                    const int f = as_global(k.slot_field)[j0 + __ffsll((unsigned long long)todo) - 1];
+        // the bags of all sequence fields, one after the other, dealt to the wavefronts (four looks at 64 fields at a time)
+        int64_t base = 0, next = blockIdx.x;
+        for (int f0 = 0; f0 < job.n_fields; f0 += 256) {
+            int lo[4], hi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t* o = offsets + (int64_t)min(f0 + 64 * i + lane, job.n_fields - 1) * job.B;
+                lo[i] = o[0]; hi[i] = o[job.B];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int f1 = f0 + 64 * i;
+                for (uint64_t todo = __ballot(f1 + lane < job.n_fields && mx_is_seq(job, (int64_t)hi[i] - lo[i])); todo; todo &= todo - 1) {
+                    const int f = f1 + __ffsll((unsigned long long)todo) - 1;
                     const FieldMeta m = as_global(job.fmeta)[f];
-                    const int32_t* offs = as_global(job.offsets) + (int64_t)f * job.B;
-                    for (; next < base + job.B; next += n_waves) {
+                    int p = 0;
+                    while (p < job.n_packs && job.pack[p].p != m.pack) ++p;
+                    if (p == job.n_packs) continue;        // another launch's
+                    const MxPack& k = job.pack[p];
+                    const int32_t* offs = offsets + (int64_t)f * job.B;
+                    for (; next < base + job.B; next += job.seq_blocks) {
                         const int b = (int)(next - base);
-#define MX_SEQ(W, M, G) mx_seq_bag<W, M, G>(job, k, m, offs, b)
+#define MX_SEQ(K) mx_seq_bag<K>(job, k, m, offs, b, s_key)
                         MX_KINDS(MX_SEQ)
                     }
                     base += job.B;
@@ -287,18 +366,27 @@ mx_lookup_kernel(MxJob job)
         }
         return;
     }
-    if (item == 0 && threadIdx.x == 0) {
-        const int32_t* o = as_global(job.offsets);
-        if (o[0] != 0 || o[(int64_t)job.n_fields * job.B] != job.nnz) atomicOr(job.error_word, 1);
+    if (item == 0 && lane == 0) {
+        if (offsets[0] != 0 || offsets[(int64_t)job.n_fields * job.B] != job.nnz) atomicOr(job.error_word, 1);
     }
     int p = 0;
     while (p + 1 < job.n_packs && item >= job.pack[p + 1].item_begin) ++p;
     const MxPack& k = job.pack[p];
-    const int j = (item - k.item_begin) / k.tiles, tile = item - k.item_begin - j * k.tiles;
+    int j, tile;
+    if (job.by_xcd) {                                      // a field's tiles on one XCD (blocks go to them in turn)
+        const int x = item & 7, i = (item - k.item_begin) >> 3, h = i / k.tiles;
+        j = 8 * h + ((x - k.turn) & 7); tile = i - h * k.tiles;
+        if (j >= k.n_fields) return;
+    } else {
+        j = (item - k.item_begin) / k.tiles; tile = item - k.item_begin - j * k.tiles;
+    }
     const int f = as_global(k.slot_field)[j];
-    if (mx_is_seq(job, f)) return;
+    const int32_t* offs = offsets + (int64_t)f * job.B;
+    const int64_t field_ids = (int64_t)offs[job.B] - offs[0];
+    if (mx_is_seq(job, field_ids)) return;
     const FieldMeta m = as_global(job.fmeta)[f];
-    const int32_t* offs = as_global(job.offsets) + (int64_t)f * job.B;
-#define MX_TILE(W, M, G) mx_tile<W, M, G>(job, k, m, offs, tile, s_bin, s_bag)
-    MX_KINDS(MX_TILE)
+#define MX_TILE8(K) mx_tile<K, 8>(job, k, m, offs, tile, s_bin, s_bag, s_key, s_out)
+#define MX_TILE1(K) mx_tile<K, 1>(job, k, m, offs, tile, s_bin, s_bag, s_key, s_out)
+    if (2 * field_ids > 5 * (int64_t)job.B) { MX_KINDS(MX_TILE8) }
+    else { MX_KINDS(MX_TILE1) }
 }

@@ -497,22 +497,21 @@ pk_status pk_mx_forward(const pk_plan* plan, const void* const* T, const int64_t
         std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return plan->packs[x].dim > plan->packs[y].dim; });
         for (size_t i = 0; i < order.size(); i += kMxPacks) {
             MxJob job{};
-            int64_t items = 0;
+            int64_t items = 0, fields = 0;
+            job.by_xcd = (int)plan->fields.size() >= kMxXcdFields;
             for (size_t o = i; o < std::min(order.size(), i + kMxPacks); ++o) {
                 const Pack& k = plan->packs[order[o]];
-                int sh = 0;
-                while ((32 << sh) < k.dim) ++sh;
-                const int kind = sh == 0 ? (k.dim + 7) / 8 : k.dim % 32 == 0 && (k.dim / 32 & (k.dim / 32 - 1)) == 0 ? 5 : 6;
-                const int tiles = (B + (NT >> sh) - 1) / (NT >> sh);
-                job.pack[job.n_packs++] = MxPack{static_cast<const uint8_t*>(T[order[o]]), ds->slot_field + k.first_slot, k.dim, sh, kind,
+                const int kind = mx_kind(k.dim), bags = 128 >> mx_lanes_shift(kind), tiles = (B + bags - 1) / bags;
+                job.pack[job.n_packs++] = MxPack{static_cast<const uint8_t*>(T[order[o]]), ds->slot_field + k.first_slot, k.dim, kind,
                                                  (int32_t)mx_row_bytes(PK_MXFP4, k.dim), (int32_t)mx_code_bytes(PK_MXFP4, k.dim),
-                                                 (int32_t)k.fields.size(), tiles, (int32_t)items};
-                items += (int64_t)k.fields.size() * tiles;
+                                                 (int32_t)k.fields.size(), tiles, (int32_t)items, (int32_t)(fields & 7), order[o]};
+                items += (int64_t)(job.by_xcd ? (k.fields.size() + 7) / 8 * 8 : k.fields.size()) * tiles;
+                fields += (int64_t)k.fields.size();
             }
-            job.B = B; job.n_fields = (int32_t)plan->fields.size(); job.n_items = (int32_t)items; job.nnz = nnz;
-            job.seq_blocks = nnz >= (int64_t)kMxSeqAvg * B ? (int)std::min<int64_t>(1024, std::max<int64_t>(1, nnz / (kMxSeqAvg * (NT / 64)))) : 0;
+            job.B = B; job.n_fields = (int32_t)plan->fields.size(); job.nnz = nnz;
+            job.seq_blocks = nnz >= (int64_t)kMxSeqAvg * B ? (int)(std::min<int64_t>(kMxSeqBlocks, nnz / kMxSeqIds + 1) + 7) / 8 * 8 : 0;
             job.fmeta = ds->fmeta; job.ids = ids; job.offsets = offsets; job.out = out; job.out_stride = out_row_stride; job.error_word = error_word;
-            PK_LAUNCH("pk_mx_lookup", mx_lookup_kernel, dim3((unsigned)(job.seq_blocks + items)), dim3(NT), 0, job);
+            PK_LAUNCH("pk_mx_lookup", mx_lookup_kernel, dim3((unsigned)(job.seq_blocks + items)), dim3(64), 0, job);
         }
         return PK_OK;
     } catch (...) { return PK_ENOMEM; }
