@@ -1,71 +1,208 @@
 // y = Q(x) W^T + bias, both operands in 4 bits.
 // Part of pk_mx.hip: included there, in this order, inside its anonymous namespace.
 
-struct LinearLayout { int64_t x_stride; size_t total; };
+// ---------------------------------------------------------------------------
+// x is rounded first, into the workspace, in the product's own layout: codes [M][kp / 2] and scale bytes [M][kp / 32], K filled up
+// with zeros (scale 1) to whole steps kp.  A block then takes kLinM x kLinN of y, kLinK of K a step: codes and scales go to
+// LDS through registers, the next step's on their way while this one is multiplied.  A scaled product of 16 x 16 x 128 takes of every
+// lane 16 bytes and a scale: row (column) l % 16 and of the 128 the block l / 16.  W is its first operand, so that a lane's four results are
+// neighbours in a row of y.  Where the tiles are too few for the chip, K is cut into stretches whose sums meet in a second
+// launch, in their order.
+// ---------------------------------------------------------------------------
+constexpr int kLinM = 128, kLinN = 128, kLinK = 256;
+constexpr int kLinRow = kLinK / 2;               // bytes of a row's codes in LDS
+constexpr int kLinStretch = 6;                   // steps of a stretch, at least
+
+struct LinearLayout { int64_t kp, tiles_m, tiles_n, steps, splits, ld; size_t scales, parts, total; };
 inline LinearLayout linear_layout(int64_t M, int64_t N, int64_t K)
 {
+    auto pad = [](int64_t b) { return (size_t)((b + 255) / 256 * 256); };
     LinearLayout L;
-    (void)N;
-    L.x_stride = (mx_row_bytes(PK_MXFP4, K) + 15) / 16 * 16;
-    L.total = std::max<size_t>(kAlign, (size_t)(M * L.x_stride) + kAlign);
+    L.steps = (K + kLinK - 1) / kLinK;
+    L.kp = L.steps * kLinK;
+    L.tiles_m = (M + kLinM - 1) / kLinM;
+    L.tiles_n = (N + kLinN - 1) / kLinN;
+    const int64_t tiles = std::max<int64_t>(1, L.tiles_m * L.tiles_n);
+    L.splits = std::max<int64_t>(1, std::min<int64_t>(L.steps / kLinStretch, 384 / tiles));
+    L.ld = (N + 3) / 4 * 4;
+    L.scales = pad(M * (L.kp / 2));
+    L.parts = L.scales + pad(M * (L.kp / 32));
+    L.total = std::max<size_t>(kAlign, L.parts + (L.splits > 1 ? pad(L.splits * M * L.ld * 4) : 0));
     return L;
+}
+
+// x's rows in the layout above; a thread takes eight columns as in mx_quantize_kernel, groups: of kp columns
+template <bool BF16>
+__global__ void __launch_bounds__(NT)
+mx_linear_round_kernel(const char* __restrict__ src, int64_t src_stride, uint32_t cols, RowGroups groups, uint32_t* __restrict__ codes,
+                       uint8_t* __restrict__ scales, int64_t items)
+{
+    for (int64_t base = (int64_t)blockIdx.x * NT; base < items; base += (int64_t)gridDim.x * NT) {
+        if (base + threadIdx.x >= items) break;
+        uint32_t g;
+        const int64_t r = groups.row(base, threadIdx.x, g);
+        float x[8];
+        load_f8<BF16>(src + r * src_stride + (int64_t)g * (BF16 ? 16 : 32), (int)cols - (int)(8 * g), x);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+        m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+        const uint32_t s = mx_scale_byte<PK_MXFP4>(m);
+        uint32_t w[1];
+        mx_encode8<PK_MXFP4>(x, s, w);
+        const int64_t at = base + threadIdx.x;             // (rows follow one another without gaps)
+        codes[at] = w[0];
+        if ((g & 3) == 0) scales[at >> 2] = (uint8_t)s;
+    }
 }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4m __attribute__((ext_vector_type(4)));
 
-// block kb of a row: its 32 codes (what lies behind the last word is zero) and its scale (1 behind the last block)
-__device__ __forceinline__ void mx_load_block(const uint8_t* row, int words, int blocks, int kb, i32x8& v, int& scale)
+// where chunk c (16 bytes) of row r stands: the eight chunks of a row trade places, so that neighbouring rows' are on different banks
+__device__ __forceinline__ int lin_at(int r, int c) { return r * kLinRow + ((c ^ r) & 7) * 16; }
+
+// four neighbours in a row of y
+template <bool BF16>
+__device__ __forceinline__ void lin_store(char* y, int64_t at, int left, const f32x4m& v)
 {
-    const uint32_t* at = reinterpret_cast<const uint32_t*>(row) + 4 * kb;
-    v = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
-    if (4 * kb + 4 <= words) {
-        uint32_t u[4];
-        load_u32<4>(at, u);
-        v[0] = (int)u[0]; v[1] = (int)u[1]; v[2] = (int)u[2]; v[3] = (int)u[3];
+    if constexpr (BF16) {
+        uint16_t* o = reinterpret_cast<uint16_t*>(y) + at;
+        const uint32_t a = pack_bf16(v[0], v[1]), b = pack_bf16(v[2], v[3]);
+        if (left >= 4) {
+            u32x2_b2 u;
+            u.x = a; u.y = b;
+            *reinterpret_cast<u32x2_b2*>(o) = u;
+        } else {
+            o[0] = (uint16_t)a;
+            if (left > 1) o[1] = (uint16_t)(a >> 16);
+            if (left > 2) o[2] = (uint16_t)b;
+        }
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (4 * kb + i < words) v[i] = (int)at[i];
+        float* o = reinterpret_cast<float*>(y) + at;
+        if (left >= 4) {
+            f32x4 u;
+            u.x = v[0]; u.y = v[1]; u.z = v[2]; u.w = v[3];
+            *reinterpret_cast<f32x4*>(o) = u;
+        } else {
+            o[0] = v[0];
+            if (left > 1) o[1] = v[1];
+            if (left > 2) o[2] = v[2];
+        }
     }
-    scale = kb < blocks ? (int)row[words * 4 + kb] : 127;
 }
 
-// A wavefront takes 16 rows and 64 columns of y: one scaled product of 16 x 16 x 128 per 16 columns and 128 of K.  Lane l holds
-// row (and column) l % 16 and of the 128 the block l / 16, so that its operand is 16 bytes and one scale byte.
 template <bool BF16>
 __global__ void __launch_bounds__(256)
-mx_linear_kernel(const uint8_t* __restrict__ xq, int64_t x_stride, const uint8_t* __restrict__ wq, int64_t w_stride, int M, int N, int K,
-                 const float* __restrict__ bias, char* __restrict__ y, int64_t y_stride)
+mx_linear_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const uint8_t* __restrict__ wq, int64_t w_stride, int M, int N, int K,
+                 int tiles_n, int tiles, int steps, int splits, const float* __restrict__ bias, char* __restrict__ y, int64_t y_stride, int64_t split_stride)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int n0 = blockIdx.x * 64, words = (K + 7) / 8, blocks = (K + 31) / 32;
-    for (int64_t m0 = (int64_t)blockIdx.y * 64 + wave * 16; m0 < M; m0 += (int64_t)gridDim.y * 64) {
-        const uint8_t* xr = xq + min(m0 + r, (int64_t)M - 1) * x_stride;
-        f32x4m acc[4] = {};
-        for (int kb = 0; kb < blocks; kb += 4) {
-            i32x8 a; int sa;
-            mx_load_block(xr, words, blocks, kb + q, a, sa);
+    __shared__ __attribute__((aligned(16))) char s_x[kLinM * kLinRow], s_w[kLinN * kLinRow];
+    __shared__ __attribute__((aligned(8))) char s_sx[kLinM * 8], s_sw[kLinN * 8];
+    // an XCD takes neighbouring pieces of the work: those of one stretch and one stretch of rows share x in its L2
+    const int n_work = tiles * splits, per = (n_work + 7) / 8, work = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || work >= n_work) return;
+    const int split = work / tiles, tile = work - split * tiles, tm = tile / tiles_n, tn = tile - tm * tiles_n;
+    const int step0 = (int)((int64_t)steps * split / splits), step1 = (int)((int64_t)steps * (split + 1) / splits);
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave & 1, wn = wave >> 1, r = lane & 15, q = lane >> 4;
+    const int kp = steps * kLinK, words = (K + 7) / 8, blocks = (K + 31) / 32;
+    // what this thread brings of a step: chunk c of rows t / 8, t / 8 + 32 ..., and the scales of row t / 2, half of its eight
+    const int c = t & 7, row = t >> 3, srow = t >> 1, half = t & 1;
+    const uint8_t* xs = scales + (int64_t)min(tm * kLinM + srow, M - 1) * (kp / 32) + 4 * half;
+    const uint8_t* ws = wq + (int64_t)min(tn * kLinN + srow, N - 1) * w_stride + 4 * (int64_t)words;
+    uint32_t x[4][4], w[4][4], sx, sw;
+    auto load = [&](int step) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                i32x8 b; int sb;
-                mx_load_block(wq + (int64_t)min(n0 + 16 * t + r, N - 1) * w_stride, words, blocks, kb + q, b, sb);
-                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[t], 4, 4, 0, sa, 0, sb);
+        for (int i = 0; i < 4; ++i) {
+            load_u32<4>(reinterpret_cast<const uint32_t*>(codes + (int64_t)min(tm * kLinM + row + 32 * i, M - 1) * (kp / 2) + (int64_t)step * kLinRow + 16 * c), x[i]);
+            const uint32_t* at = reinterpret_cast<const uint32_t*>(wq + (int64_t)min(tn * kLinN + row + 32 * i, N - 1) * w_stride);
+            const int first = step * (kLinRow / 4) + 4 * c;
+            if (first + 4 <= words) {
+                load_u32<4>(at + first, w[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { w[i][j] = 0; if (first + j < words) w[i][j] = at[first + j]; }
             }
         }
+        sx = *reinterpret_cast<const uint32_t*>(xs + step * 8);
+        const int b = step * 8 + 4 * half;                 // (the row's scales fill whole words)
+        sw = b < blocks ? *reinterpret_cast<const uint32_t*>(ws + b) : 0u;
+    };
+    auto store = [&]() {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int n = n0 + 16 * t + r;
-            if (n >= N) continue;
-            const float add = bias ? bias[n] : 0.f;
+        for (int i = 0; i < 4; ++i) {
+            *reinterpret_cast<uint4*>(s_x + lin_at(row + 32 * i, c)) = make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]);
+            *reinterpret_cast<uint4*>(s_w + lin_at(row + 32 * i, c)) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+        }
+        *reinterpret_cast<uint32_t*>(s_sx + srow * 8 + 4 * half) = sx;
+        *reinterpret_cast<uint32_t*>(s_sw + srow * 8 + 4 * half) = sw;
+    };
+    f32x4m acc[4][4] = {};                                 // [columns of y][rows of y]
+    if (step0 < step1) load(step0);
+    for (int step = step0; step < step1; ++step) {
+        store();
+        __syncthreads();
+        if (step + 1 < step1) load(step + 1);
+        uint2 fsx[4], fsw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            fsx[i] = *reinterpret_cast<const uint2*>(s_sx + (wm * 64 + i * 16 + r) * 8);
+            fsw[i] = *reinterpret_cast<const uint2*>(s_sw + (wn * 64 + i * 16 + r) * 8);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            i32x8 fx[4], fw[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int64_t m = m0 + 4 * q + i;
-                if (m >= M) continue;
-                const float v = acc[t][i] + add;
-                if constexpr (BF16) reinterpret_cast<uint16_t*>(y)[m * y_stride + n] = (uint16_t)pack_bf16(v, 0.f);
-                else reinterpret_cast<float*>(y)[m * y_stride + n] = v;
+                const uint4 a = *reinterpret_cast<const uint4*>(s_x + lin_at(wm * 64 + i * 16 + r, 4 * h + q));
+                const uint4 b = *reinterpret_cast<const uint4*>(s_w + lin_at(wn * 64 + i * 16 + r, 4 * h + q));
+                fx[i] = i32x8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
+                fw[i] = i32x8{(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i], fx[j], acc[i][j], 4, 4, 0, (int)((h ? fsw[i].y : fsw[i].x) >> (8 * q)),
+                                                                                0, (int)((h ? fsx[j].y : fsx[j].x) >> (8 * q)));
         }
+        __syncthreads();
+    }
+    y += split * split_stride;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int n = tn * kLinN + wn * 64 + i * 16 + 4 * q;
+        if (n >= N) continue;
+        f32x4m add = {0.f, 0.f, 0.f, 0.f};
+        if (bias)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) add[e] = bias[min(n + e, N - 1)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int m = tm * kLinM + wm * 64 + j * 16 + r;
+            if (m < M) lin_store<BF16>(y, m * y_stride + n, N - n, acc[i][j] + add);
+        }
+    }
+}
+
+// the stretches' sums, added up in their order, and the bias
+template <bool BF16>
+__global__ void __launch_bounds__(NT)
+mx_linear_join_kernel(const float* __restrict__ part, int64_t ld, int64_t split_stride, int splits, int N, int64_t items, const float* __restrict__ bias,
+                      char* __restrict__ y, int64_t y_stride)
+{
+    const int64_t per_row = ld / 4;
+    for (int64_t it = (int64_t)blockIdx.x * NT + threadIdx.x; it < items; it += (int64_t)gridDim.x * NT) {
+        const int64_t m = it / per_row;
+        const int n = (int)(it - m * per_row) * 4;
+        const float* p = part + m * ld + n;
+        f32x4 v = *reinterpret_cast<const f32x4*>(p);
+        for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * split_stride);
+        f32x4m u = {v.x, v.y, v.z, v.w};
+        if (bias)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] += bias[min(n + e, N - 1)];
+        lin_store<BF16>(y, m * y_stride + n, N - n, u);
     }
 }

@@ -50,6 +50,7 @@ const char* bad_rows(const void* p, int32_t format, int64_t stride, int64_t n_ro
 pk_status bad_shape(const char* who, const char* what) { return fail(PK_ESHAPE, std::string(who) + ": " + what); }
 
 constexpr int64_t kMxMax = ((int64_t)1 << 31) - 1;      // rows, columns
+constexpr int64_t kMxProductMax = (int64_t)1 << 30;      // sizes of a product (they are filled up to whole tiles in 32 bits)
 
 template <int FMT, bool BF16>
 pk_status quantize_launch(const void* src, int64_t src_stride, int64_t n_rows, int64_t cols, void* rows, int64_t row_stride, hipStream_t stream)
@@ -77,11 +78,15 @@ pk_status guarded(Fn&& fn) noexcept
     try { return fn(); } catch (...) { return PK_ENOMEM; }
 }
 
-pk_status check_matrix_shape(const char* who, int64_t n_rows, int64_t cols)
+pk_status check_matrix_shape(const char* who, int64_t n_rows, int64_t cols, int64_t most = kMxMax)
 {
     if (n_rows < 0 || cols <= 0) return bad_shape(who, "sizes must be positive (rows may be 0)");
-    if (n_rows > kMxMax || cols > kMxMax) return fail(PK_EOVERFLOW, std::string(who) + ": sizes must be below 2^31");
+    if (n_rows > most || cols > most) return fail(PK_EOVERFLOW, std::string(who) + ": sizes must be at most " + std::to_string(most));
     return PK_OK;
+}
+bool bad_product(int64_t rows, int64_t N, int64_t K)
+{
+    return rows < 0 || N <= 0 || K <= 0 || rows > kMxProductMax || N > kMxProductMax || K > kMxProductMax;
 }
 
 }  // namespace
@@ -132,7 +137,7 @@ pk_status pk_mx_dequantize(const void* rows, int64_t row_stride, int64_t n_rows,
 
 size_t pk_mx_linear_workspace_bytes(int64_t M, int64_t N, int64_t K)
 {
-    if (M < 0 || N <= 0 || K <= 0 || M > kMxMax || N > kMxMax || K > kMxMax) { set_error("pk_mx_linear_workspace_bytes: bad sizes"); return 0; }
+    if (bad_product(M, N, K)) { set_error("pk_mx_linear_workspace_bytes: bad sizes"); return 0; }
     return linear_layout(M, N, K).total;
 }
 
@@ -142,8 +147,8 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
 {
     return guarded([&]() -> pk_status {
         const char* who = "pk_mx_linear";
-        pk_status rc = check_matrix_shape(who, M, K);
-        if (rc == PK_OK) rc = check_matrix_shape(who, N, K);
+        pk_status rc = check_matrix_shape(who, M, K, kMxProductMax);
+        if (rc == PK_OK) rc = check_matrix_shape(who, N, K, kMxProductMax);
         if (rc != PK_OK) return rc;
         if (N == 0) return bad_shape(who, "N must be positive");
         const char* bad = bad_matrix(x, x_dtype, x_row_stride, M, K);
@@ -157,20 +162,34 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
         if (misaligned(workspace, kAlign)) return fail(PK_EWORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
         if (ws_bytes < L.total) return fail(PK_EWORKSPACE, std::string(who) + ": workspace is smaller than pk_mx_linear_workspace_bytes");
         hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-        uint8_t* xq = static_cast<uint8_t*>(workspace);
-        rc = (x_dtype == PK_BF16 ? quantize_launch<PK_MXFP4, true> : quantize_launch<PK_MXFP4, false>)(x, x_row_stride, M, K, xq, L.x_stride, stream);
-        if (rc != PK_OK) return rc;
-        const dim3 grid((unsigned)((N + 63) / 64), (unsigned)std::min<int64_t>((M + 63) / 64, 65535));
-        const auto kernel = y_dtype == PK_BF16 ? mx_linear_kernel<true> : mx_linear_kernel<false>;
-        MX_LAUNCH("mx_linear", kernel, grid, dim3(256), xq, L.x_stride, static_cast<const uint8_t*>(w_rows), w_row_stride, (int)M, (int)N, (int)K,
-                  bias, static_cast<char*>(y), y_row_stride);
+        char* ws = static_cast<char*>(workspace);
+        const RowGroups g(L.kp);
+        const int64_t items = M * g.n, tiles = L.tiles_m * L.tiles_n;
+        if (tiles * L.splits > ((int64_t)1 << 30)) return fail(PK_EOVERFLOW, std::string(who) + ": M * N is too large");
+        uint32_t* codes = reinterpret_cast<uint32_t*>(ws);
+        uint8_t* scales = reinterpret_cast<uint8_t*>(ws + L.scales);
+        const auto round = x_dtype == PK_BF16 ? mx_linear_round_kernel<true> : mx_linear_round_kernel<false>;
+        MX_LAUNCH("mx_linear_round", round, dim3(mx_blocks_for(items)), dim3(NT), static_cast<const char*>(x), x_row_stride * (x_dtype == PK_BF16 ? 2 : 4), (uint32_t)K,
+                  g, codes, scales, items);
+        const bool join = L.splits > 1;
+        char* parts = ws + L.parts;
+        const auto kernel = y_dtype == PK_BF16 && !join ? mx_linear_kernel<true> : mx_linear_kernel<false>;
+        MX_LAUNCH("mx_linear", kernel, dim3((unsigned)((tiles * L.splits + 7) / 8 * 8)), dim3(256), reinterpret_cast<const uint8_t*>(codes), scales,
+                  static_cast<const uint8_t*>(w_rows), w_row_stride, (int)M, (int)N, (int)K, (int)L.tiles_n, (int)tiles, (int)L.steps, (int)L.splits,
+                  join ? nullptr : bias, join ? parts : static_cast<char*>(y), join ? L.ld : y_row_stride, M * L.ld * 4);
+        if (join) {
+            const int64_t n = M * (L.ld / 4);
+            const auto sum = y_dtype == PK_BF16 ? mx_linear_join_kernel<true> : mx_linear_join_kernel<false>;
+            MX_LAUNCH("mx_linear_join", sum, dim3(mx_blocks_for(n)), dim3(NT), reinterpret_cast<const float*>(parts), L.ld, M * L.ld, (int)L.splits, (int)N, n,
+                      bias, static_cast<char*>(y), y_row_stride);
+        }
         return PK_OK;
     });
 }
 
 size_t pk_mx_weight_grad_workspace_bytes(int64_t B, int64_t N, int64_t K)
 {
-    if (B < 0 || N <= 0 || K <= 0 || B > kMxMax || N > kMxMax || K > kMxMax) { set_error("pk_mx_weight_grad_workspace_bytes: bad sizes"); return 0; }
+    if (bad_product(B, N, K)) { set_error("pk_mx_weight_grad_workspace_bytes: bad sizes"); return 0; }
     return grad_layout(B, N, K).total;
 }
 
@@ -180,8 +199,8 @@ pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_str
 {
     return guarded([&]() -> pk_status {
         const char* who = "pk_mx_weight_grad";
-        pk_status rc = check_matrix_shape(who, B, K);
-        if (rc == PK_OK) rc = check_matrix_shape(who, B, N);
+        pk_status rc = check_matrix_shape(who, B, K, kMxProductMax);
+        if (rc == PK_OK) rc = check_matrix_shape(who, B, N, kMxProductMax);
         if (rc != PK_OK) return rc;
         const char* bad = bad_matrix(dy, dy_dtype, dy_row_stride, B, N);
         if (!bad) bad = bad_rows(x_rows, PK_MXFP8, x_row_stride, B, K);
