@@ -319,7 +319,8 @@ pk_status pk_partition_unique(const pk_plan* plan, const void* workspace, size_t
  * stride are multiples of 16 are read faster by pk_mx_linear and pk_mx_weight_grad.
  *
  * Matrices of fp32 or bf16: element-aligned, row stride in elements, >= the columns
- * (not looked at for one row).  Sizes below 2^31, of products at most 2^30.  Calls with no rows do nothing
+ * (not looked at for one row).  Sizes below 2^31; of products at
+ * most 2^30, K at most 2^23 and the microscaled rows at most 2^24 bytes apart.  Calls with no rows do nothing
  * (pk_mx_weight_grad: the sum over no samples).  These calls need no plan, allocate
  * nothing and only enqueue work on hip_stream, which belongs to the current device;
  * workspaces are the caller's, and calls that may run at the same time (two streams,

@@ -11,6 +11,7 @@
 // ---------------------------------------------------------------------------
 constexpr int kLinM = 128, kLinN = 128, kLinK = 256;
 constexpr int kLinRow = kLinK / 2;               // bytes of a row's codes in LDS
+constexpr int kLinScales = 16;                   // steps whose scales are in LDS at a time: 128 bytes a row
 constexpr int kLinStretch = 6;                   // steps of a stretch, at least
 
 struct LinearLayout { int64_t kp, tiles_m, tiles_n, steps, splits, ld; size_t scales, parts, total; };
@@ -23,7 +24,7 @@ inline LinearLayout linear_layout(int64_t M, int64_t N, int64_t K)
     L.tiles_m = (M + kLinM - 1) / kLinM;
     L.tiles_n = (N + kLinN - 1) / kLinN;
     const int64_t tiles = std::max<int64_t>(1, L.tiles_m * L.tiles_n);
-    L.splits = std::max<int64_t>(1, std::min<int64_t>(L.steps / kLinStretch, 384 / tiles));
+    L.splits = std::max<int64_t>(1, std::min<int64_t>(L.steps / kLinStretch, 512 / tiles));
     L.ld = (N + 3) / 4 * 4;
     L.scales = pad(M * (L.kp / 2));
     L.parts = L.scales + pad(M * (L.kp / 32));
@@ -98,8 +99,9 @@ __global__ void __launch_bounds__(256)
 mx_linear_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const uint8_t* __restrict__ wq, int64_t w_stride, int M, int N, int K,
                  int tiles_n, int tiles, int steps, int splits, const float* __restrict__ bias, char* __restrict__ y, int64_t y_stride, int64_t split_stride)
 {
-    __shared__ __attribute__((aligned(16))) char s_x[kLinM * kLinRow], s_w[kLinN * kLinRow];
-    __shared__ __attribute__((aligned(8))) char s_sx[kLinM * 8], s_sw[kLinN * 8];
+    __shared__ __attribute__((aligned(16))) char s_all[4][128 * 128];
+    static_assert(kLinM == 128 && kLinN == 128 && kLinRow == 128 && 8 * kLinScales == 128, "a row's codes and its scales are 128 bytes each");
+    char *s_x = s_all[0], *s_w = s_all[1], *s_sx = s_all[2], *s_sw = s_all[3];
     // an XCD takes neighbouring pieces of the work: those of one stretch and one stretch of rows share x in its L2
     const int n_work = tiles * splits, per = (n_work + 7) / 8, work = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || work >= n_work) return;
@@ -107,27 +109,34 @@ mx_linear_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ 
     const int step0 = (int)((int64_t)steps * split / splits), step1 = (int)((int64_t)steps * (split + 1) / splits);
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave & 1, wn = wave >> 1, r = lane & 15, q = lane >> 4;
     const int kp = steps * kLinK, words = (K + 7) / 8, blocks = (K + 31) / 32;
-    // what this thread brings of a step: chunk c of rows t / 8, t / 8 + 32 ..., and the scales of row t / 2, half of its eight
-    const int c = t & 7, row = t >> 3, srow = t >> 1, half = t & 1;
-    const uint8_t* xs = scales + (int64_t)min(tm * kLinM + srow, M - 1) * (kp / 32) + 4 * half;
-    const uint8_t* ws = wq + (int64_t)min(tn * kLinN + srow, N - 1) * w_stride + 4 * (int64_t)words;
-    uint32_t x[4][4], w[4][4], sx, sw;
+    // what this thread brings of a step: chunk c of rows t / 8, t / 8 + 32 ...
+    const int c = t & 7, row = t >> 3;
+    uint32_t x[4][4], w[4][4];
+    // (a tile's rows are less than 2^31 bytes apart: kMxDepthMax)
+    const uint8_t* xt = codes + (int64_t)tm * kLinM * (kp / 2);
+    const uint8_t* wt = wq + (int64_t)tn * kLinN * w_stride;
+    uint32_t xo[4], wo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        xo[i] = (uint32_t)min(row + 32 * i, M - 1 - tm * kLinM) * (uint32_t)(kp / 2) + 16 * c;
+        wo[i] = (uint32_t)min(row + 32 * i, N - 1 - tn * kLinN) * (uint32_t)w_stride + 16 * c;
+    }
     auto load = [&](int step) {
+        const uint8_t *xb = xt + (int64_t)step * kLinRow, *wb = wt + (int64_t)step * kLinRow;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            load_u32<4>(reinterpret_cast<const uint32_t*>(codes + (int64_t)min(tm * kLinM + row + 32 * i, M - 1) * (kp / 2) + (int64_t)step * kLinRow + 16 * c), x[i]);
-            const uint32_t* at = reinterpret_cast<const uint32_t*>(wq + (int64_t)min(tn * kLinN + row + 32 * i, N - 1) * w_stride);
-            const int first = step * (kLinRow / 4) + 4 * c;
-            if (first + 4 <= words) {
-                load_u32<4>(at + first, w[i]);
-            } else {
+        for (int i = 0; i < 4; ++i) load_u32<4>(reinterpret_cast<const uint32_t*>(xb + xo[i]), x[i]);
+        if ((step + 1) * (kLinK / 8) <= words) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) { w[i][j] = 0; if (first + j < words) w[i][j] = at[first + j]; }
-            }
+            for (int i = 0; i < 4; ++i) load_u32<4>(reinterpret_cast<const uint32_t*>(wb + wo[i]), w[i]);
+        } else {                                           // the last step of a row that does not fill it
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[i][j] = 0;
+                    if (step * (kLinK / 8) + 4 * c + j < words) w[i][j] = reinterpret_cast<const uint32_t*>(wb + wo[i])[j];
+                }
         }
-        sx = *reinterpret_cast<const uint32_t*>(xs + step * 8);
-        const int b = step * 8 + 4 * half;                 // (the row's scales fill whole words)
-        sw = b < blocks ? *reinterpret_cast<const uint32_t*>(ws + b) : 0u;
     };
     auto store = [&]() {
 #pragma unroll
@@ -135,20 +144,43 @@ mx_linear_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ 
             *reinterpret_cast<uint4*>(s_x + lin_at(row + 32 * i, c)) = make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]);
             *reinterpret_cast<uint4*>(s_w + lin_at(row + 32 * i, c)) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
         }
-        *reinterpret_cast<uint32_t*>(s_sx + srow * 8 + 4 * half) = sx;
-        *reinterpret_cast<uint32_t*>(s_sw + srow * 8 + 4 * half) = sw;
+    };
+    // The scales of kLinScales steps, in whole lines: eight bytes of a row a step are a request each, and an L1 has few on their way.
+    // Step i's eight bytes of row r stand at place i ^ r of the row.
+    auto load_scales = [&](int first) {
+        const int word = 2 * first + (t & 31);
+        const bool in_x = word < kp / 128, in_w = 4 * word < blocks;
+#pragma nounroll
+        for (int h = 0; h < 16; h += 8) {
+            uint32_t v[8], u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int rr = (t >> 5) + 8 * (h + i);
+                v[i] = u[i] = 0;
+                if (in_x) v[i] = *reinterpret_cast<const uint32_t*>(scales + (int64_t)min(tm * kLinM + rr, M - 1) * (kp / 32) + 4 * word);
+                if (in_w) u[i] = *reinterpret_cast<const uint32_t*>(wt + (uint32_t)min(rr, N - 1 - tn * kLinN) * (uint32_t)w_stride + 4 * (words + word));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int rr = (t >> 5) + 8 * (h + i), at = rr * 8 * kLinScales + ((((t & 31) >> 1) ^ rr) & (kLinScales - 1)) * 8 + (t & 1) * 4;
+                *reinterpret_cast<uint32_t*>(s_sx + at) = v[i];
+                *reinterpret_cast<uint32_t*>(s_sw + at) = u[i];
+            }
+        }
     };
     f32x4m acc[4][4] = {};                                 // [columns of y][rows of y]
     if (step0 < step1) load(step0);
     for (int step = step0; step < step1; ++step) {
+        const int place = (step - step0) & (kLinScales - 1);
+        if (place == 0) load_scales(step);
         store();
         __syncthreads();
         if (step + 1 < step1) load(step + 1);
         uint2 fsx[4], fsw[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            fsx[i] = *reinterpret_cast<const uint2*>(s_sx + (wm * 64 + i * 16 + r) * 8);
-            fsw[i] = *reinterpret_cast<const uint2*>(s_sw + (wn * 64 + i * 16 + r) * 8);
+            fsx[i] = *reinterpret_cast<const uint2*>(s_sx + (wm * 64 + i * 16 + r) * 8 * kLinScales + (place ^ r) * 8);
+            fsw[i] = *reinterpret_cast<const uint2*>(s_sw + (wn * 64 + i * 16 + r) * 8 * kLinScales + (place ^ r) * 8);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -169,20 +201,27 @@ mx_linear_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ 
         }
         __syncthreads();
     }
+    // y by way of LDS, so that a wavefront writes whole rows of the tile (16 rows of 32 bytes at a time: 6 us more for 17 MB); the
+    // 32 chunks of a row trade places
     y += split * split_stride;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int n = tn * kLinN + wn * 64 + i * 16 + 4 * q;
-        if (n >= N) continue;
-        f32x4m add = {0.f, 0.f, 0.f, 0.f};
-        if (bias)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) add[e] = bias[min(n + e, N - 1)];
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int m = tm * kLinM + wm * 64 + j * 16 + r;
-            if (m < M) lin_store<BF16>(y, m * y_stride + n, N - n, acc[i][j] + add);
+            const int m = wm * 64 + j * 16 + r, chunk = wn * 16 + i * 4 + q;
+            *reinterpret_cast<f32x4m*>(s_all[0] + m * 512 + (chunk ^ (m & 31)) * 16) = acc[i][j];
         }
+    __syncthreads();
+    const int chunk = t & 31, n = tn * kLinN + 4 * chunk;
+    if (n >= N) return;
+    f32x4m add = {0.f, 0.f, 0.f, 0.f};
+    if (bias)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) add[e] = bias[min(n + e, N - 1)];
+#pragma unroll 4
+    for (int k = 0; k < 16; ++k) {
+        const int row_y = (t >> 5) + 8 * k, m = tm * kLinM + row_y;
+        if (m < M) lin_store<BF16>(y, m * y_stride + n, N - n, *reinterpret_cast<const f32x4m*>(s_all[0] + row_y * 512 + (chunk ^ (row_y & 31)) * 16) + add);
     }
 }
 

@@ -50,7 +50,9 @@ const char* bad_rows(const void* p, int32_t format, int64_t stride, int64_t n_ro
 pk_status bad_shape(const char* who, const char* what) { return fail(PK_ESHAPE, std::string(who) + ": " + what); }
 
 constexpr int64_t kMxMax = ((int64_t)1 << 31) - 1;      // rows, columns
-constexpr int64_t kMxProductMax = (int64_t)1 << 30;      // sizes of a product (they are filled up to whole tiles in 32 bits)
+// Products: rows and columns of the result (whole tiles of them are counted in 32 bits); columns of microscaled rows and bytes
+// between them (a tile's 128 rows are addressed in 32 bits).
+constexpr int64_t kMxProductMax = (int64_t)1 << 30, kMxDepthMax = (int64_t)1 << 23;
 
 template <int FMT, bool BF16>
 pk_status quantize_launch(const void* src, int64_t src_stride, int64_t n_rows, int64_t cols, void* rows, int64_t row_stride, hipStream_t stream)
@@ -78,15 +80,22 @@ pk_status guarded(Fn&& fn) noexcept
     try { return fn(); } catch (...) { return PK_ENOMEM; }
 }
 
-pk_status check_matrix_shape(const char* who, int64_t n_rows, int64_t cols, int64_t most = kMxMax)
+pk_status check_matrix_shape(const char* who, int64_t n_rows, int64_t cols)
 {
     if (n_rows < 0 || cols <= 0) return bad_shape(who, "sizes must be positive (rows may be 0)");
-    if (n_rows > most || cols > most) return fail(PK_EOVERFLOW, std::string(who) + ": sizes must be at most " + std::to_string(most));
+    if (n_rows > kMxMax || cols > kMxMax) return fail(PK_EOVERFLOW, std::string(who) + ": sizes must be below 2^31");
+    return PK_OK;
+}
+pk_status check_product(const char* who, int64_t rows, int64_t N, int64_t K, int64_t row_stride)
+{
+    if (rows < 0 || N <= 0 || K <= 0) return bad_shape(who, "sizes must be positive (rows of the input may be 0)");
+    if (rows > kMxProductMax || N > kMxProductMax) return fail(PK_EOVERFLOW, std::string(who) + ": rows and N must be at most 2^30");
+    if (K > kMxDepthMax || row_stride > kMxDepthMax * 2) return fail(PK_EOVERFLOW, std::string(who) + ": K must be at most 2^23, microscaled rows at most 2^24 bytes apart");
     return PK_OK;
 }
 bool bad_product(int64_t rows, int64_t N, int64_t K)
 {
-    return rows < 0 || N <= 0 || K <= 0 || rows > kMxProductMax || N > kMxProductMax || K > kMxProductMax;
+    return rows < 0 || N <= 0 || K <= 0 || rows > kMxProductMax || N > kMxProductMax || K > kMxDepthMax;
 }
 
 }  // namespace
@@ -147,10 +156,8 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
 {
     return guarded([&]() -> pk_status {
         const char* who = "pk_mx_linear";
-        pk_status rc = check_matrix_shape(who, M, K, kMxProductMax);
-        if (rc == PK_OK) rc = check_matrix_shape(who, N, K, kMxProductMax);
+        pk_status rc = check_product(who, M, N, K, w_row_stride);
         if (rc != PK_OK) return rc;
-        if (N == 0) return bad_shape(who, "N must be positive");
         const char* bad = bad_matrix(x, x_dtype, x_row_stride, M, K);
         if (!bad) bad = bad_matrix(y, y_dtype, y_row_stride, M, N);
         if (!bad) bad = bad_rows(w_rows, PK_MXFP4, w_row_stride, N, K);
@@ -199,8 +206,7 @@ pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_str
 {
     return guarded([&]() -> pk_status {
         const char* who = "pk_mx_weight_grad";
-        pk_status rc = check_matrix_shape(who, B, K, kMxProductMax);
-        if (rc == PK_OK) rc = check_matrix_shape(who, B, N, kMxProductMax);
+        const pk_status rc = check_product(who, B, N, K, x_row_stride);
         if (rc != PK_OK) return rc;
         const char* bad = bad_matrix(dy, dy_dtype, dy_row_stride, B, N);
         if (!bad) bad = bad_rows(x_rows, PK_MXFP8, x_row_stride, B, K);
