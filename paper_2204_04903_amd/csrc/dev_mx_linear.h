@@ -14,6 +14,11 @@ constexpr int kLinRow = kLinK / 2;               // bytes of a row's codes in LD
 constexpr int kLinScales = 16;                   // steps whose scales are in LDS at a time: 128 bytes a row
 constexpr int kLinStretch = 6;                   // steps of a stretch, at least
 
+// Few rows of x, up to 16 of kLinFew elements together, take one launch (K 832, N 1024, 1 and 16 rows: 4.2 and 5.1 us, by tiles 10.5 and
+// 10.8; K 3840, 16 rows 10.7 and 15.0; K 6000 and 16 rows 15.3 both; K 12000, N 1024, 1, 4, 8 rows 13.8 17.7 21.5, by tiles 16.3 16.4 16.7:
+// each block reads all of x).
+constexpr int64_t kLinFew = 1 << 16;
+inline bool linear_few(int64_t M, int64_t K) { return M <= 16 && M * K <= kLinFew; }
 struct LinearLayout { int64_t kp, tiles_m, tiles_n, steps, splits, ld; size_t scales, parts, total; };
 inline LinearLayout linear_layout(int64_t M, int64_t N, int64_t K)
 {
@@ -28,7 +33,7 @@ inline LinearLayout linear_layout(int64_t M, int64_t N, int64_t K)
     L.ld = (N + 3) / 4 * 4;
     L.scales = pad(M * (L.kp / 2));
     L.parts = L.scales + pad(M * (L.kp / 32));
-    L.total = std::max<size_t>(kAlign, L.parts + (L.splits > 1 ? pad(L.splits * M * L.ld * 4) : 0));
+    L.total = linear_few(M, K) ? kAlign : std::max<size_t>(kAlign, L.parts + (L.splits > 1 ? pad(L.splits * M * L.ld * 4) : 0));
     return L;
 }
 
@@ -243,5 +248,79 @@ mx_linear_join_kernel(const float* __restrict__ part, int64_t ld, int64_t split_
 #pragma unroll
             for (int e = 0; e < 4; ++e) u[e] += bias[min(n + e, N - 1)];
         lin_store<BF16>(y, m * y_stride + n, N - n, u);
+    }
+}
+
+// Few rows of x: a block takes 16 columns of y and all of K, its wavefronts a stretch each; x is rounded in registers, a lane
+// a block of 32 of its row, just as the product wants it.  The stretches' sums meet in LDS, in their order.
+template <bool XBF, bool YBF>
+__global__ void __launch_bounds__(1024)
+mx_linear_few_kernel(const char* __restrict__ x, int64_t x_stride, int M, const uint8_t* __restrict__ wq, int64_t w_stride, int N, int K,
+                     const float* __restrict__ bias, char* __restrict__ y, int64_t y_stride)
+{
+    __shared__ float s_part[16][16][17];                   // [wavefront][row of x][column]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, r = lane & 15, q = lane >> 4;
+    const int n0 = blockIdx.x * 16, words = (K + 7) / 8, blocks = (K + 31) / 32, steps = (blocks + 3) / 4;
+    const uint8_t* wr = wq + (int64_t)min(n0 + r, N - 1) * w_stride;
+    const char* xr = x + (int64_t)min(r, M - 1) * x_stride;
+    f32x4m acc = {0.f, 0.f, 0.f, 0.f};
+    struct Step { uint32_t w[4], s; float x[4][8]; };
+    // WHOLE: the step lies inside the rows.  (Lanes of rows that are not there read the last one; what they give is not written.)
+    auto load = [&](Step& v, int step, auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        const int kb = 4 * step + q;
+        if (WHOLE || 4 * kb + 4 <= words) {
+            load_u32<4>(reinterpret_cast<const uint32_t*>(wr) + 4 * kb, v.w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v.w[i] = 0; if (4 * kb + i < words) v.w[i] = reinterpret_cast<const uint32_t*>(wr)[4 * kb + i]; }
+        }
+        v.s = 127;
+        if (WHOLE || kb < blocks) v.s = wr[4 * words + kb];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_f8<XBF>(xr + (int64_t)(32 * kb + 8 * i) * (XBF ? 2 : 4), WHOLE ? 8 : K - 32 * kb - 8 * i, v.x[i]);
+    };
+    auto multiply = [&](const Step& v) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v.x[i][j]) & 0x7FFFFFFFu);
+        const uint32_t s = mx_scale_byte<PK_MXFP4>(m);
+        const i32x8 a = {(int)v.w[0], (int)v.w[1], (int)v.w[2], (int)v.w[3], 0, 0, 0, 0};
+        i32x8 b = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w[1];
+            mx_encode8<PK_MXFP4>(v.x[i], s, w);
+            b[i] = (int)w[0];
+        }
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, 0, (int)v.s, 0, (int)s);
+    };
+    const int first = steps * wave / waves, end = steps * (wave + 1) / waves, whole = min(end, K / 128);
+    int step = first;
+    for (; step + 2 <= whole; step += 2) {
+        Step v0, v1;
+        load(v0, step, std::true_type{});
+        load(v1, step + 1, std::true_type{});
+        multiply(v0);
+        multiply(v1);
+    }
+    for (; step < end; ++step) {
+        Step v;
+        load(v, step, std::false_type{});
+        multiply(v);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s_part[wave][r][4 * q + i] = acc[i];
+    __syncthreads();
+    for (int at = threadIdx.x; at < 16 * 16; at += blockDim.x) {
+        const int m = at >> 4, c = at & 15, n = n0 + c;
+        if (m >= M || n >= N) continue;
+        float v = s_part[0][m][c];
+        for (int w = 1; w < waves; ++w) v += s_part[w][m][c];
+        if (bias) v += bias[n];
+        if constexpr (YBF) reinterpret_cast<uint16_t*>(y)[m * y_stride + n] = (uint16_t)pack_bf16(v, 0.f);
+        else reinterpret_cast<float*>(y)[m * y_stride + n] = v;
     }
 }

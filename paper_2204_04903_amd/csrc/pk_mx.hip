@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "pk_internal.h"
 
@@ -169,6 +170,15 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
         if (misaligned(workspace, kAlign)) return fail(PK_EWORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
         if (ws_bytes < L.total) return fail(PK_EWORKSPACE, std::string(who) + ": workspace is smaller than pk_mx_linear_workspace_bytes");
         hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+        const int64_t x_bytes = x_row_stride * (x_dtype == PK_BF16 ? 2 : 4);
+        if (linear_few(M, K)) {
+            const int waves = (int)std::min<int64_t>(16, std::max<int64_t>(1, (K + 255) / 256));
+            const auto few = x_dtype == PK_BF16 ? (y_dtype == PK_BF16 ? mx_linear_few_kernel<true, true> : mx_linear_few_kernel<true, false>)
+                                                : (y_dtype == PK_BF16 ? mx_linear_few_kernel<false, true> : mx_linear_few_kernel<false, false>);
+            MX_LAUNCH("mx_linear_few", few, dim3((unsigned)((N + 15) / 16)), dim3(64 * waves), static_cast<const char*>(x), x_bytes, (int)M,
+                      static_cast<const uint8_t*>(w_rows), w_row_stride, (int)N, (int)K, bias, static_cast<char*>(y), y_row_stride);
+            return PK_OK;
+        }
         char* ws = static_cast<char*>(workspace);
         const RowGroups g(L.kp);
         const int64_t items = M * g.n, tiles = L.tiles_m * L.tiles_n;
@@ -176,7 +186,7 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
         uint32_t* codes = reinterpret_cast<uint32_t*>(ws);
         uint8_t* scales = reinterpret_cast<uint8_t*>(ws + L.scales);
         const auto round = x_dtype == PK_BF16 ? mx_linear_round_kernel<true> : mx_linear_round_kernel<false>;
-        MX_LAUNCH("mx_linear_round", round, dim3(mx_blocks_for(items)), dim3(NT), static_cast<const char*>(x), x_row_stride * (x_dtype == PK_BF16 ? 2 : 4), (uint32_t)K,
+        MX_LAUNCH("mx_linear_round", round, dim3(mx_blocks_for(items)), dim3(NT), static_cast<const char*>(x), x_bytes, (uint32_t)K,
                   g, codes, scales, items);
         const bool join = L.splits > 1;
         char* parts = ws + L.parts;
