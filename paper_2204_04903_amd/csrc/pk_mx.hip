@@ -227,7 +227,7 @@ pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_str
         if (ws_bytes < pk_mx_weight_grad_workspace_bytes(B, N, K)) return fail(PK_EWORKSPACE, std::string(who) + ": workspace is smaller than pk_mx_weight_grad_workspace_bytes");
         hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         const GradLayout L = grad_layout(B, N, K);
-        const int64_t tiles = L.tiles_n * L.tiles_k;
+        const int64_t tiles = L.tiles;
         if (tiles * L.splits > ((int64_t)1 << 30)) return fail(PK_EOVERFLOW, std::string(who) + ": N * K is too large");
         const bool join = L.splits > 1;
         const auto kernel = dy_dtype == PK_BF16 ? mx_grad_kernel<false> : mx_grad_kernel<true>;

@@ -184,21 +184,32 @@ def _device(device) -> torch.device:
     return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
 
 
-def _matrix(x: torch.Tensor, name: str, shape, device, dtypes=tuple(_MX_DTYPE)) -> int:
+def _matrix(x: torch.Tensor, name: str, rows: int, cols: int, device, dtypes=_MX_DTYPE) -> int:
     """Checks a matrix argument; returns its row stride in elements."""
-    if x.dim() != 2 or tuple(x.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(x.shape)}")
+    if x.dim() != 2 or x.shape[0] != rows or x.shape[1] != cols:
+        raise ValueError(f"{name} must be [{rows}, {cols}], got {list(x.shape)}")
     if x.dtype not in dtypes:
-        raise ValueError(f"{name} must be one of {dtypes}, got {x.dtype}")
+        raise ValueError(f"{name} must be one of {list(dtypes)}, got {x.dtype}")
     if x.device != device:
         raise ValueError(f"{name} is on {x.device}, expected {device}")
-    if x.numel() == 0:
-        return x.shape[1]
-    if x.shape[1] > 1 and x.stride(1) != 1:
+    s0, s1 = x.stride()
+    if rows == 0 or cols == 0:
+        return cols
+    if cols > 1 and s1 != 1:
         raise ValueError(f"{name}: neighbouring columns must be neighbours in memory")
-    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+    if rows > 1 and s0 < cols:
         raise ValueError(f"{name}: rows overlap")
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return s0 if rows > 1 else cols
+
+
+def _enqueue(device, call, *args) -> None:
+    """The library's call on the device's current stream, with the device current."""
+    stream = torch.cuda.current_stream(device.index).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        call(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            call(*args, stream)
 
 
 class MxRows:
@@ -225,19 +236,15 @@ class MxRows:
         self.data, self.stride = data, stride
 
     def quantize(self, x: torch.Tensor) -> "MxRows":
-        xs = _matrix(x, "x", (self.n_rows, self.cols), self.device)
-        with torch.cuda.device(self.device):
-            pk.pk_mx_quantize(x, _MX_DTYPE[x.dtype], xs, self.n_rows, self.cols, self.format, self.data, self.stride,
-                              torch.cuda.current_stream().cuda_stream)
+        stride = _matrix(x, "x", self.n_rows, self.cols, self.device)
+        _enqueue(self.device, pk.pk_mx_quantize, x, _MX_DTYPE[x.dtype], stride, self.n_rows, self.cols, self.format, self.data, self.stride)
         return self
 
     def dequantize(self, out: torch.Tensor = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
         if out is None:
             out = torch.empty((self.n_rows, self.cols), dtype=dtype, device=self.device)
-        os_ = _matrix(out, "out", (self.n_rows, self.cols), self.device)
-        with torch.cuda.device(self.device):
-            pk.pk_mx_dequantize(self.data, self.stride, self.n_rows, self.cols, self.format, out, _MX_DTYPE[out.dtype], os_,
-                                torch.cuda.current_stream().cuda_stream)
+        stride = _matrix(out, "out", self.n_rows, self.cols, self.device)
+        _enqueue(self.device, pk.pk_mx_dequantize, self.data, self.stride, self.n_rows, self.cols, self.format, out, _MX_DTYPE[out.dtype], stride)
         return out
 
 
@@ -256,17 +263,16 @@ class ActivationCheckpoint(MxRows):
         if grad_y.dim() != 2:
             raise ValueError("grad_y must have two dimensions")
         N = int(grad_y.shape[1])
-        gs = _matrix(grad_y, "grad_y", (self.n_rows, N), self.device)
+        grad_stride = _matrix(grad_y, "grad_y", self.n_rows, N, self.device)
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs out")
             out = torch.empty((N, self.cols), dtype=torch.float32, device=self.device)
-        os_ = _matrix(out, "out", (N, self.cols), self.device, (torch.float32,))
-        with torch.cuda.device(self.device):
-            ws_bytes = pk.pk_mx_weight_grad_workspace_bytes(self.n_rows, N, self.cols)
-            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)       # (the allocator's: free again when the stream is past it)
-            pk.pk_mx_weight_grad(grad_y, _MX_DTYPE[grad_y.dtype], gs, self.data, self.stride, self.n_rows, N, self.cols, out, os_,
-                                 accumulate, ws, ws_bytes, torch.cuda.current_stream().cuda_stream)
+        out_stride = _matrix(out, "out", N, self.cols, self.device, (torch.float32,))
+        ws_bytes = pk.pk_mx_weight_grad_workspace_bytes(self.n_rows, N, self.cols)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)       # (the allocator's: free again when the stream is past it)
+        _enqueue(self.device, pk.pk_mx_weight_grad, grad_y, _MX_DTYPE[grad_y.dtype], grad_stride, self.data, self.stride, self.n_rows, N, self.cols,
+                 out, out_stride, accumulate, ws, ws_bytes)
         return out
 
 
@@ -299,15 +305,14 @@ class QuantizedLinear:
         if x.dim() != 2:
             raise ValueError("x must have two dimensions")
         M = int(x.shape[0])
-        xs = _matrix(x, "x", (M, self.K), self.device)
+        x_stride = _matrix(x, "x", M, self.K, self.device)
         if out is None:
             out = torch.empty((M, self.N), dtype=dtype, device=self.device)
-        os_ = _matrix(out, "out", (M, self.N), self.device)
-        with torch.cuda.device(self.device):
-            ws_bytes = pk.pk_mx_linear_workspace_bytes(M, self.N, self.K)
-            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
-            pk.pk_mx_linear(x, _MX_DTYPE[x.dtype], xs, M, self.weight.data, self.weight.stride, self.N, self.K, self.bias, out,
-                            _MX_DTYPE[out.dtype], os_, ws, ws_bytes, torch.cuda.current_stream().cuda_stream)
+        out_stride = _matrix(out, "out", M, self.N, self.device)
+        ws_bytes = pk.pk_mx_linear_workspace_bytes(M, self.N, self.K)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+        _enqueue(self.device, pk.pk_mx_linear, x, _MX_DTYPE[x.dtype], x_stride, M, self.weight.data, self.weight.stride, self.N, self.K, self.bias, out,
+                 _MX_DTYPE[out.dtype], out_stride, ws, ws_bytes)
         return out
 
 
@@ -338,6 +343,7 @@ class QuantizedEmbedding:
         for m in self.T:
             if m.stride != pk.pk_mx_row_bytes(m.format, m.cols):
                 raise ValueError("a pack's rows must be pk_mx_row_bytes apart")
+        self._T = [m.data for m in self.T]
         self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
 
     @classmethod
@@ -369,10 +375,8 @@ class QuantizedEmbedding:
                 raise ValueError(f"{name} must be contiguous {dt} on {self.device}" + (f", {n} of them" if n is not None else ""))
         if out is None:
             out = torch.empty((B, self.out_dim), dtype=torch.float32, device=self.device)
-        stride = _matrix(out, "out", (B, self.out_dim), self.device, (torch.float32,))
-        with torch.cuda.device(self.device):
-            pk.pk_mx_forward(self.plan, [m.data for m in self.T], ids, offsets, B, int(ids.shape[0]), out, stride, self.error,
-                             torch.cuda.current_stream().cuda_stream)
+        stride = _matrix(out, "out", B, self.out_dim, self.device, (torch.float32,))
+        _enqueue(self.device, pk.pk_mx_forward, self.plan, self._T, ids, offsets, B, ids.shape[0], out, stride, self.error)
         return out
 
     def error_word(self) -> int:
