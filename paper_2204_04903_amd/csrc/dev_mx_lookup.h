@@ -18,7 +18,7 @@
 // ---------------------------------------------------------------------------
 constexpr int kMxPacks = 16;     // packs of one launch
 constexpr int kMxSeqAvg = 64;
-constexpr int64_t kMxSeqBlocks = 4096, kMxSeqIds = 512;      // wavefronts for their bags, at most, and IDs that there should be for each
+constexpr int64_t kMxSeqBlocks = 8192, kMxSeqIds = 512;      // wavefronts for their bags, at most, and IDs that there should be for each
 constexpr int kMxXcdFields = 32; // fields from which every one has its XCD
 constexpr int kMxBins = 32;      // numbers of rounds that are told apart
 struct MxPack {
@@ -51,11 +51,14 @@ struct MxSrc {
 template <int KIND>
 struct MxLane {
     static constexpr int W = KIND == 0 ? 1 : 2, SH = mx_lanes_shift(KIND), L = 1 << SH, G = 64 >> SH;
-    int c, sh0, sh1;                                       // first word; where the words' scales are in the scale word
-    __device__ __forceinline__ explicit MxLane(int code_bytes)
+    int c;                                                 // first word
+    uint32_t turn0, turn1;                                 // the words' scales, turned to where a number has its exponent
+    const uint8_t *at, *scale_at;
+    __device__ __forceinline__ explicit MxLane(const MxSrc& src)
     {
-        c = KIND == 0 ? 0 : min(2 * (int)(threadIdx.x & (L - 1)), (code_bytes >> 2) - 2);
-        sh0 = (c >> 2) * 8; sh1 = ((c + 1) >> 2) * 8;
+        c = KIND == 0 ? 0 : min(2 * (int)(threadIdx.x & (L - 1)), (src.code_bytes >> 2) - 2);
+        turn0 = ((c >> 2) * 8 + 9) & 31; turn1 = (((c + 1) >> 2) * 8 + 9) & 31;
+        at = src.T + 4 * c; scale_at = src.T + src.code_bytes;
     }
     // the rows of R keys in LDS, of which `left` count
     template <int R>
@@ -64,32 +67,42 @@ struct MxLane {
         uint32_t w[R][W], s[R], s2[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const uint8_t* row = src.T + (size_t)s_key[i] * src.stride;
-            const uint32_t* at = reinterpret_cast<const uint32_t*>(row) + c;
+            const uint64_t row = (uint64_t)s_key[i] * src.stride;
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(at + row);
             if constexpr (W == 1) {
                 uint32_t v[2];
-                load_u32<2>(at, v);
+                load_u32<2>(p, v);
                 w[i][0] = v[0]; s[i] = v[1];
             } else if constexpr (KIND == 5) {
                 uint32_t v[2];
-                load_u32<2>(at, v);
+                load_u32<2>(p, v);
                 w[i][0] = v[0]; w[i][1] = v[1];
-                s[i] = row[src.code_bytes + (c >> 2)]; s2[i] = row[src.code_bytes + ((c + 1) >> 2)];
+                s[i] = scale_at[row + (c >> 2)]; s2[i] = scale_at[row + ((c + 1) >> 2)];
             } else {
                 typedef uint32_t u32x3 __attribute__((ext_vector_type(3), aligned(4)));
-                const u32x3 v = *reinterpret_cast<const u32x3*>(at);
+                const u32x3 v = *reinterpret_cast<const u32x3*>(p);
                 w[i][0] = v.x; w[i][1] = v.y; s[i] = v.z;
             }
         }
+        // (of a scale operand the exponent is all that is read: what else the word holds may stay)
         float f0[R], f1[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             if constexpr (KIND == 2) s[i] = (uint32_t)__builtin_amdgcn_mov_dpp((int)s[i], 0xF5, 0xF, 0xF, true);        // lanes 1 1 3 3
             if constexpr (KIND == 3) s[i] = (uint32_t)__builtin_amdgcn_mov_dpp((int)s[i], 0xFF, 0xF, 0xF, true);        // lane 3
             if constexpr (KIND == 4) s[i] = (uint32_t)__shfl((int)s[i], threadIdx.x | 7, 64);
-            f0[i] = mx_scale((KIND == 5 ? s[i] : KIND <= 1 ? s[i] : s[i] >> sh0) & 255u);
-            f1[i] = mx_scale((KIND == 5 ? s2[i] : KIND <= 1 ? s[i] : s[i] >> sh1) & 255u);
-            if (i > 0)                                     // past the bag's end: nothing (its last row again, whose scale does no harm)
+            if constexpr (KIND == 5) {
+                f0[i] = mx_scale(s[i]); f1[i] = mx_scale(s2[i]);
+            } else if constexpr (KIND <= 1) {
+                f0[i] = f1[i] = mx_scale(s[i]);
+            } else {
+                f0[i] = __uint_as_float(__builtin_amdgcn_alignbit(s[i], s[i], turn0));
+                f1[i] = __uint_as_float(__builtin_amdgcn_alignbit(s[i], s[i], turn1));
+            }
+        }
+        if (__any(left < R)) {                             // past the bag's end: nothing (its last row again, whose scale does no harm)
+#pragma unroll
+            for (int i = 1; i < R; ++i)
 #pragma unroll
                 for (int j = 0; j < W; ++j) w[i][j] = i < left ? w[i][j] : 0;
         }
@@ -180,7 +193,7 @@ __device__ __forceinline__ void mx_tile(const MxJob& job, const MxPack& k, const
     mx_bag(job, offs, bag2, R == 1 && 2 * G - 1 - g < nb, q2, e2);
     int todo = (g < nb) + (g < nb && 2 * G - 1 - g < nb);  // bags that this group has left to write
     if (todo == 0) q = e = 0;
-    const Lane me(src.code_bytes);
+    const Lane me(src);
     int q0 = q;                                            // where the bag begins
     double acc[8 * W] = {};
     // the IDs of a round: lane l reads number l % R of groups l / R, l / R + 64 / R ...
@@ -272,7 +285,7 @@ __device__ __forceinline__ void mx_seq_bag(const MxJob& job, const MxPack& k, co
     const MxSrc src(job, k, m);
     int q0, e;
     mx_bag(job, offs, b, lane == 0, q0, e);
-    const Lane me(src.code_bytes);
+    const Lane me(src);
     double acc[C] = {};
     int64_t id[N];
     auto ask = [&](int at) {
