@@ -363,7 +363,7 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
 
 /* The gradient of a dense layer's weights from the 8-bit checkpoint of its input:
  *   dw[n, k] (+)= sum_b dy[b, n] * X[b, k]
- * dy: device, fp32 or bf16 [B, dy_row_stride] (fp32 numbers are multiplied in full);
+ * dy: device, fp32 or bf16 [B, dy_row_stride], N and the stride at most 2^24 (fp32 numbers are multiplied in full);
  * x_rows: device, B rows of K columns, PK_MXFP8;  dw: device, fp32 [N, dw_row_stride].
  * accumulate: 0 = dw is overwritten, else added to (micro-batches).  Sums in fp32, in an
  * order that depends on the sizes only: the same call gives the same bits.

@@ -54,6 +54,7 @@ constexpr int64_t kMxMax = ((int64_t)1 << 31) - 1;      // rows, columns
 // Products: rows and columns of the result (whole tiles of them are counted in 32 bits); columns of microscaled rows and bytes
 // between them (a tile's 128 rows are addressed in 32 bits).
 constexpr int64_t kMxProductMax = (int64_t)1 << 30, kMxDepthMax = (int64_t)1 << 23;
+constexpr int64_t kMxGradStrideMax = (int64_t)1 << 24;   // elements between rows of dY (16 rows are addressed in 31 bits)
 
 template <int FMT, bool BF16>
 pk_status quantize_launch(const void* src, int64_t src_stride, int64_t n_rows, int64_t cols, void* rows, int64_t row_stride, hipStream_t stream)
@@ -218,6 +219,7 @@ pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_str
         const char* who = "pk_mx_weight_grad";
         const pk_status rc = check_product(who, B, N, K, x_row_stride);
         if (rc != PK_OK) return rc;
+        if (N > kMxGradStrideMax || (B > 1 && dy_row_stride > kMxGradStrideMax)) return fail(PK_EOVERFLOW, std::string(who) + ": N and the distance of dy's rows must be at most 2^24");
         const char* bad = bad_matrix(dy, dy_dtype, dy_row_stride, B, N);
         if (!bad) bad = bad_rows(x_rows, PK_MXFP8, x_row_stride, B, K);
         if (!bad) bad = bad_matrix(dw, PK_F32, dw_row_stride, N, K);
@@ -230,11 +232,11 @@ pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_str
         const int64_t tiles = L.tiles;
         if (tiles * L.splits > ((int64_t)1 << 30)) return fail(PK_EOVERFLOW, std::string(who) + ": N * K is too large");
         const bool join = L.splits > 1;
-        const auto kernel = dy_dtype == PK_BF16 ? mx_grad_kernel<false> : mx_grad_kernel<true>;
-        MX_LAUNCH("mx_grad", kernel, dim3((unsigned)((tiles * L.splits + 7) / 8 * 8)), dim3(256), static_cast<const char*>(dy),
-                  dy_row_stride * (dy_dtype == PK_BF16 ? 2 : 4), static_cast<const uint8_t*>(x_rows), x_row_stride, B, (int)N, (int)K, (int)L.tiles_n,
-                  (int)tiles, (int)L.steps, (int)L.splits, join ? static_cast<float*>(workspace) : dw, join ? L.ld : dw_row_stride, N * L.ld,
-                  join ? 0 : accumulate);
+        const GradJob job{static_cast<const char*>(dy), (B > 1 ? dy_row_stride : N) * (dy_dtype == PK_BF16 ? 2 : 4), static_cast<const uint8_t*>(x_rows), x_row_stride, B,
+                          (int)N, (int)K, (int)L.tiles_n, (int)tiles, (int)L.steps, (int)L.splits, join ? static_cast<float*>(workspace) : dw,
+                          join ? L.ld : dw_row_stride, N * L.ld, join ? 0 : accumulate};
+        const auto kernel = dy_dtype == PK_BF16 ? mx_grad_bf16_kernel : mx_grad_f32_kernel;
+        MX_LAUNCH("mx_grad", kernel, dim3((unsigned)((tiles * L.splits + 7) / 8 * 8)), dim3(256), job);
         if (join) {
             const int64_t items = N * (L.ld / 4);
             MX_LAUNCH("mx_grad_join", mx_grad_join_kernel, dim3(mx_blocks_for(items)), dim3(NT), static_cast<const float*>(workspace), L.ld, N * L.ld,
