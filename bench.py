@@ -103,6 +103,9 @@ def parse_args():
     ap.add_argument("--partition", type=int, default=0,
                     help="also time Partition (Sec. II-D) of every pack's distinct keys over this many owners, after "
                          "the timed steps, and report the sizes of the owners' groups and what Shuffle would carry")
+    ap.add_argument("--serve-4bit", action="store_true",
+                    help="also round the tables to 4 bits after the timed steps and time the pooled lookup of the batches "
+                         "from them, beside the forward pass that training takes")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="also run one plain 1 GiB device copy (a known size for scaling rocprofv3's byte counters)")
@@ -302,6 +305,29 @@ def run_workload(args, workload):
         raise RuntimeError(f"{workload}: the device error word is {layer.error_word()} after the timed steps")
 
     # ---- Partition of the last step's distinct keys (outside the timed steps) ----------------------
+    serve_info = None
+    if args.serve_4bit and not hybrid:
+        from paper_2204_04903_amd.layer import QuantizedEmbedding
+        serve = QuantizedEmbedding.from_layer(layer, **plan_opts)
+
+        def per_batch(call):
+            call(0)
+            torch.cuda.synchronize()
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for i in range(5 * ring):
+                call(i % ring)
+            b.record()
+            torch.cuda.synchronize()
+            return a.elapsed_time(b) / (5 * ring)
+        ms4 = per_batch(lambda i: serve.forward(dev[i][0], dev[i][1], wl.batch, out=out))
+        ms = per_batch(lambda i: layer.forward(dev[i][0], dev[i][1], wl.batch, out=out))
+        mean_nnz = sum(b.nnz for b in batches) / ring
+        serve_info = {"ms_per_batch": ms4, "lookups_per_s": mean_nnz / ms4 * 1e3, "forward_ms_per_batch": ms,
+                      "table_bytes": sum(int(m.data.numel()) for m in serve.T),
+                      "full_table_bytes": sum(int(w.numel()) * w.element_size() for w in layer.W), "error_word": serve.error_word()}
+        serve.close()
+
     partition_info = None
     if args.partition > 0 and not hybrid:
         n_own = args.partition
@@ -368,6 +394,7 @@ def run_workload(args, workload):
         "hybrid_hash": hybrid_info,
         "d_interleaving": micro_info,
         "partition": partition_info,
+        **({"serve_4bit": serve_info} if serve_info else {}),
         "kernels": {k: {kk: round(vv, 6) for kk, vv in v.items()} for k, v in kern.items()},
         "input_generation_s": round(gen_s, 2),
     }

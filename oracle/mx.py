@@ -16,11 +16,11 @@ def row_bytes(fmt, cols):
 
 
 def scale_exponent(top, fmt):
-    """smallest t >= -126 with top <= 2^t * MAX"""
-    most, t = GRID[fmt][-1], -126
-    while top > most * 2.0 ** t:
-        t += 1
-    return t
+    """smallest t >= -126 with top <= 2^t * MAX (numbers or arrays)"""
+    most, top = GRID[fmt][-1], np.asarray(top, np.float64)
+    t = np.maximum(np.ceil(np.log2(np.maximum(top, 2.0 ** -140) / most)), -126.0)
+    t = np.where((t > -126) & (top <= most * 2.0 ** (t - 1)), t - 1, t)          # (the logarithm is rounded: its neighbours are looked at)
+    return np.where(top > most * 2.0 ** t, t + 1, t).astype(np.int64)
 
 
 def nearest(u, fmt):
@@ -40,17 +40,13 @@ def encode(x, fmt):
     out = np.zeros((R, row_bytes(fmt, C)), np.uint8)
     codes = np.zeros((R, (C + 31) // 32 * 32), np.uint8)
     for b in range((C + 31) // 32):
-        blk = x[:, 32 * b:32 * b + 32]
-        for r in range(R):
-            v = blk[r]
-            if not np.isfinite(v).all():
-                out[r, n + b] = 255
-                codes[r, 32 * b:32 * b + 32] = 0 if fmt == MXFP4 else 0x7F
-                continue
-            t = scale_exponent(np.abs(v).max(), fmt)
-            out[r, n + b] = t + 127
-            sign = np.signbit(v).astype(np.uint8)
-            codes[r, 32 * b:32 * b + len(v)] = nearest(np.abs(v) / 2.0 ** t, fmt) | sign << (3 if fmt == MXFP4 else 7)
+        v = x[:, 32 * b:32 * b + 32]
+        bad = ~np.isfinite(v).all(1)
+        t = scale_exponent(np.where(bad, 1.0, np.abs(v).max(1)), fmt)
+        out[:, n + b] = np.where(bad, 255, t + 127)
+        u = np.where(bad[:, None], 0.0, np.abs(v)) / 2.0 ** t[:, None].astype(np.float64)
+        c = nearest(u, fmt) | np.signbit(v).astype(np.int64) << (3 if fmt == MXFP4 else 7)
+        codes[:, 32 * b:32 * b + v.shape[1]] = np.where(bad[:, None], 0 if fmt == MXFP4 else 0x7F, c)
     if fmt == MXFP4:
         codes = codes[:, 0::2] | codes[:, 1::2] << 4
     out[:, :n] = codes[:, :n]

@@ -44,6 +44,10 @@ mx_quantize_kernel(const char* __restrict__ src, int64_t src_stride, uint32_t co
         const uint32_t s = mx_scale_byte<FMT>(m);
         uint32_t w[W];
         mx_encode8<FMT>(x, s, w);
+        if (FMT == PK_MXFP8 && n < 8) {                    // (a bad block's codes are not zeros: none behind the last column)
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = n >= 4 * i + 4 ? w[i] : n > 4 * i ? w[i] & ((1u << 8 * (n - 4 * i)) - 1u) : 0u;
+        }
         uint8_t* row = rows + r * row_stride;
         const uint32_t words = FMT == PK_MXFP4 ? (cols + 7) / 8 : (cols + 3) / 4;
         uint32_t* at = reinterpret_cast<uint32_t*>(row);

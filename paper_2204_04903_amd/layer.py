@@ -204,6 +204,8 @@ def _matrix(x: torch.Tensor, name: str, rows: int, cols: int, device, dtypes=_MX
 
 def _enqueue(device, call, *args) -> None:
     """The library's call on the device's current stream, with the device current."""
+    if device.type != "cuda":
+        raise ValueError(f"the library computes on a GPU, not on {device}")
     stream = torch.cuda.current_stream(device.index).cuda_stream
     if torch.cuda.current_device() == device.index:
         call(*args, stream)

@@ -142,6 +142,48 @@ def test_rejected_offsets(place, value, dim, max_len):
         layer.close()
 
 
+def test_a_pack_past_four_gigabytes():
+    from paper_2204_04903_amd.layer import MxRows, QuantizedEmbedding
+    rows, n = 600_000_000, 1000                          # rows of 8 bytes; only the first and the last ones are filled
+    layer = QuantizedEmbedding([(5, 8, 0), (rows, 8, 0)], [(1, 0), (0, 1)])
+    try:
+        small, tail = np.random.default_rng(1).standard_normal((5, 8)).astype(np.float32), np.random.default_rng(2).standard_normal((n, 8)).astype(np.float32)
+        layer.load_table(0, torch.from_numpy(small))
+        MxRows(n, 8, 0, data=layer.T[0].data[-n:]).quantize(torch.from_numpy(tail).cuda())
+        B = 300
+        ids = np.concatenate([np.random.default_rng(3).integers(rows - n, rows, 2 * B), np.arange(B) % 5])
+        offs = np.concatenate([np.arange(0, 2 * B, 2), 2 * B + np.arange(B + 1)]).astype(np.int32)
+        out = layer.forward(torch.from_numpy(ids).cuda(), torch.from_numpy(offs).cuda(), B).cpu().numpy()
+        dt, ds = mx.decode(mx.encode(tail, 0), 0, 8), mx.decode(mx.encode(small, 0), 0, 8)
+        a = dt[ids[:2 * B] - (rows - n)].reshape(B, 2, 8)
+        ref, mag = np.concatenate([a.sum(1), ds[np.arange(B) % 5]], 1), np.concatenate([np.abs(a).sum(1), np.abs(ds[np.arange(B) % 5])], 1)
+        assert close(out, ref, mag) and layer.error_word() == 0
+    finally:
+        layer.close()
+
+
+def test_calls_on_two_streams_at_once():
+    prs = [small_problem(60 + i, B=500, tables=[(9000, 32, 0), (700, 8, 0)], fields=[(0, 0), (1, 1), (0, 1)], max_len=30) for i in range(2)]
+    layer, dec = layer_of(prs[0])
+    try:
+        ins = [(torch.from_numpy(p["ids"]).cuda(), torch.from_numpy(p["offsets"]).cuda()) for p in prs]
+        outs = [[torch.empty((500, layer.out_dim), device="cuda") for _ in range(4)] for _ in prs]
+        streams = [torch.cuda.Stream() for _ in prs]
+        torch.cuda.synchronize()
+        for r in range(4):                               # one layer, no state of a call's own
+            for s, (ids, offs), out in zip(streams, ins, outs):
+                with torch.cuda.stream(s):
+                    layer.forward(ids, offs, 500, out=out[r])
+        torch.cuda.synchronize()
+        for p, out in zip(prs, outs):
+            ref, mag = pooled(dict(p, Wt=prs[0]["Wt"]), dec)
+            for o in out:
+                assert close(o.cpu().numpy(), ref, mag)
+        assert layer.error_word() == 0
+    finally:
+        layer.close()
+
+
 def test_layer_refuses():
     from paper_2204_04903_amd.layer import HybridEmbedding, QuantizedEmbedding
     layer = QuantizedEmbedding([(64, 4, 0)], [(0, 0)])

@@ -102,6 +102,14 @@ def test_extremes(fmt, dtype):
     check(x.to(DT[dtype]), fmt)
 
 
+@pytest.mark.parametrize("C", [1, 3, 5, 6, 7, 33, 38, 39, 70])
+def test_bad_blocks_end_with_the_last_column(C):
+    x = torch.ones(4, C)
+    x[1, C - 1], x[2, 0] = float("nan"), float("inf")
+    check(x, 0)
+    check(x, 1)
+
+
 def test_rows_past_four_gigabytes():
     from paper_2204_04903_amd.layer import MxRows
     R, C = 34_000_000, 32                               # 4.35 GB of fp32

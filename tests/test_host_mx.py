@@ -71,6 +71,8 @@ def test_linear_refuses():
         assert linear(M=M, N=N, K=K) == pk.PK_ESHAPE
     for M, N, K in ((2 ** 31, 8, 64), (4, 2 ** 31, 64), (4, 8, 2 ** 31)):
         assert linear(M=M, N=N, K=K) == pk.PK_EOVERFLOW
+    assert linear(K=2 ** 23 + 1, ws=2 ** 23) == linear(ws=2 ** 24 + 4) == linear(N=2 ** 30 + 1) == linear(M=2 ** 30 + 1) == pk.PK_EOVERFLOW
+    assert linear(M=2 ** 30, N=2 ** 30, nbytes=2 ** 62) == pk.PK_EOVERFLOW
     for bad in (dict(x=None), dict(y=None), dict(w=None), dict(work=None), dict(xdt=5), dict(ydt=-1), dict(xs=63), dict(ys=7), dict(ws=32),
                 dict(ws=50), dict(w=FAKE + 1), dict(bias=FAKE + 2), dict(x=FAKE + 1), dict(y=FAKE + 1)):
         assert linear(**bad) == pk.PK_EINVAL, bad
@@ -96,6 +98,8 @@ def test_weight_grad_refuses():
     for bad in (dict(dy=None), dict(x=None), dict(dw=None), dict(work=None), dict(dt=3), dict(ds=7), dict(xs=64), dict(xs=70), dict(dws=63),
                 dict(dw=FAKE + 2), dict(dy=FAKE + 1), dict(x=FAKE + 2)):
         assert grad(**bad) == pk.PK_EINVAL, bad
+    assert grad(ds=2 ** 24 + 1) == grad(N=2 ** 24 + 1, ds=2 ** 25) == grad(K=2 ** 23 + 1, xs=2 ** 24) == grad(xs=2 ** 24 + 4) == pk.PK_EOVERFLOW
+    assert grad(N=2 ** 24, K=2 ** 23, dws=2 ** 23, xs=2 ** 23 + 2 ** 18, nbytes=2 ** 60) == pk.PK_EOVERFLOW     # more tiles than a launch has
     assert grad(work=FAKE + 128) == pk.PK_EWORKSPACE
     assert grad(nbytes=pk.pk_mx_weight_grad_workspace_bytes(4, 8, 64) - 1) == pk.PK_EWORKSPACE
     assert status(pk.pk_mx_weight_grad_workspace_bytes, 4, 8, 0) == pk.PK_EINVAL
@@ -131,6 +135,8 @@ def test_layer_refuses_matrices_that_do_not_fit():
             MxRows(6, 40, pk.PK_MXFP4, device="cpu", data=data)
     with pytest.raises(pk.PkError):
         MxRows(6, 40, 3, device="cpu")
+    with pytest.raises(ValueError):
+        m.quantize(torch.zeros(6, 40))                   # memory of the host
     kept = ActivationCheckpoint(6, 40, device="cpu")
     for g in (torch.zeros(5, 3), torch.zeros(6), torch.zeros(6, 3, dtype=torch.float64)):
         with pytest.raises(ValueError):
