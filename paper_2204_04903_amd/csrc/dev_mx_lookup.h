@@ -17,9 +17,16 @@
 // lane giving away half of its columns a step.
 // ---------------------------------------------------------------------------
 constexpr int kMxPacks = 16;     // packs of one launch
-constexpr int kMxSeqAvg = 64;
+// From which average a field's bags go to wavefronts of their own, by the number of bags.  Few bags are too few tiles for the chip: one sample
+// of 26 fields of 32 columns takes 5.6 us at 6 IDs a bag by tiles and 5.7 by bags, 6.7 and 6.0 at 8, 12.6 and 6.1 at 50; 128 samples of 30
+// fields 13.0 and 12.7 at 8, 27 and 13.4 at 50.  Many keep the tiles busy: 1024 samples of 26 fields 32.8 and 56 at 63 IDs a bag.
+constexpr int kMxSeqAvg = 64, kMxSeqAvgFew = 8;
+constexpr int64_t kMxFewBags = 4096;
 constexpr int64_t kMxSeqBlocks = 8192, kMxSeqIds = 512;      // wavefronts for their bags, at most, and IDs that there should be for each
 constexpr int kMxXcdFields = 32; // fields from which every one has its XCD
+// One-hot bags of this many samples and more are written by tiles too: 26 fields of 32 columns, 8192 samples, 17.2 us bag by bag, 15.3 so;
+// 100 of 16 columns and 2 IDs, 1024 samples, 10.2 and 10.9; 26 of 32, 64 samples, 4.8 and 5.6.
+constexpr int kMxStagedBags = 4096;
 constexpr int kMxBins = 32;      // numbers of rounds that are told apart
 struct MxPack {
     const uint8_t* T; const int32_t* slot_field;
@@ -28,7 +35,7 @@ struct MxPack {
 };
 struct MxJob {
     MxPack pack[kMxPacks];
-    int32_t n_packs, B, n_fields, by_xcd, seq_blocks; int64_t nnz;
+    int32_t n_packs, B, n_fields, by_xcd, seq_avg, seq_blocks; int64_t nnz;
     const FieldMeta* fmeta; const int64_t* ids; const int32_t* offsets;
     float* out; int64_t out_stride; int32_t* error_word;
 };
@@ -136,7 +143,7 @@ __device__ __forceinline__ void mx_wave_order()
 }
 __device__ __forceinline__ bool mx_is_seq(const MxJob& job, int64_t field_ids)
 {
-    return job.seq_blocks && field_ids >= (int64_t)kMxSeqAvg * job.B;
+    return job.seq_blocks && field_ids >= (int64_t)job.seq_avg * job.B;
 }
 // bag b of a field: its positions, none and the error raised where its offsets are no range of the IDs
 __device__ __forceinline__ void mx_bag(const MxJob& job, const int32_t* offs, int b, bool report, int& q, int& e)
@@ -155,7 +162,7 @@ __device__ __forceinline__ void mx_tile(const MxJob& job, const MxPack& k, const
 {
     using Lane = MxLane<KIND>;
     constexpr int G = Lane::G, W = Lane::W, SH = Lane::SH, COLS = 8 * W * Lane::L;
-    constexpr bool STAGED = R > 1;                         // (sums go out together; one-hot bags as they are done)
+    const bool staged = R > 1 || job.B >= kMxStagedBags;   // sums go out together, else each as it is done
     const int lane = threadIdx.x, b0 = tile * 2 * G, nb = min(2 * G, job.B - b0);
     const MxSrc src(job, k, m);
     // the bags by their number of rounds, most first
@@ -214,13 +221,20 @@ __device__ __forceinline__ void mx_tile(const MxJob& job, const MxPack& k, const
     };
     auto write = [&]() {
         const double scale = m.pool == PK_MEAN && e > q0 ? 1.0 / (double)(e - q0) : 1.0;
-        float* o = STAGED ? s_out + (bag - b0) * COLS + 8 * me.c : as_global(job.out) + (size_t)bag * (size_t)job.out_stride + m.col + 8 * me.c;
+        float y[8 * W];
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            float y[8];
+        for (int i = 0; i < 8 * W; ++i) { y[i] = (float)(acc[i] * scale); acc[i] = 0.0; }
+        if (staged) {
+            float* o = s_out + (bag - b0) * COLS + 8 * me.c;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { y[i] = (float)(acc[8 * j + i] * scale); acc[8 * j + i] = 0.0; }
-            store_f8<false>(reinterpret_cast<char*>(o + 8 * j), STAGED ? 8 : k.D - 8 * (me.c + j), y);
+            for (int i = 0; i < 8 * W; i += 4) { f32x4 v; v.x = y[i]; v.y = y[i + 1]; v.z = y[i + 2]; v.w = y[i + 3]; *reinterpret_cast<f32x4*>(o + i) = v; }
+        } else {
+            float* o = as_global(job.out) + (size_t)bag * (size_t)job.out_stride + m.col + 8 * me.c;
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                const float z[8] = {y[8 * j], y[8 * j + 1], y[8 * j + 2], y[8 * j + 3], y[8 * j + 4], y[8 * j + 5], y[8 * j + 6], y[8 * j + 7]};
+                store_f8<false>(reinterpret_cast<char*>(o + 8 * j), k.D - 8 * (me.c + j), z);
+            }
         }
         --todo;
         bag = bag2;
@@ -241,7 +255,7 @@ __device__ __forceinline__ void mx_tile(const MxJob& job, const MxPack& k, const
             else q += R;
         }
     }
-    if (!STAGED) return;
+    if (!staged) return;
     mx_wave_order();
     // rows of the output in whole, 16 bytes a lane
     constexpr int PER = COLS / 4;
@@ -361,17 +375,19 @@ mx_lookup_kernel(MxJob job)
             for (int i = 0; i < 4; ++i) {
                 const int f1 = f0 + 64 * i;
                 for (uint64_t todo = __ballot(f1 + lane < job.n_fields && mx_is_seq(job, (int64_t)hi[i] - lo[i])); todo; todo &= todo - 1) {
-                    const int f = f1 + __ffsll((unsigned long long)todo) - 1;
-                    const FieldMeta m = as_global(job.fmeta)[f];
-                    int p = 0;
-                    while (p < job.n_packs && job.pack[p].p != m.pack) ++p;
-                    if (p == job.n_packs) continue;        // another launch's
-                    const MxPack& k = job.pack[p];
-                    const int32_t* offs = offsets + (int64_t)f * job.B;
-                    for (; next < base + job.B; next += job.seq_blocks) {
-                        const int b = (int)(next - base);
+                    if (next < base + job.B) {             // (a field's metadata only where one of its bags is this wavefront's)
+                        const int f = f1 + __ffsll((unsigned long long)todo) - 1;
+                        const FieldMeta m = as_global(job.fmeta)[f];
+                        int p = 0;
+                        while (p < job.n_packs && job.pack[p].p != m.pack) ++p;
+                        const MxPack& k = job.pack[min(p, job.n_packs - 1)];
+                        const int32_t* offs = offsets + (int64_t)f * job.B;
+                        for (; next < base + job.B; next += job.seq_blocks) {
+                            if (p == job.n_packs) continue;        // another launch's
+                            const int b = (int)(next - base);
 #define MX_SEQ(K) mx_seq_bag<K>(job, k, m, offs, b, s_key)
-                        MX_KINDS(MX_SEQ)
+                            MX_KINDS(MX_SEQ)
+                        }
                     }
                     base += job.B;
                 }

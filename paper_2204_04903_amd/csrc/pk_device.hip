@@ -509,7 +509,10 @@ pk_status pk_mx_forward(const pk_plan* plan, const void* const* T, const int64_t
                 fields += (int64_t)k.fields.size();
             }
             job.B = B; job.n_fields = (int32_t)plan->fields.size(); job.nnz = nnz;
-            job.seq_blocks = nnz >= (int64_t)kMxSeqAvg * B ? (int)(std::min<int64_t>(kMxSeqBlocks, nnz / kMxSeqIds + 1) + 7) / 8 * 8 : 0;
+            const int64_t n_bags = (int64_t)plan->fields.size() * B;
+            const bool few = n_bags <= kMxFewBags;
+            job.seq_avg = few ? kMxSeqAvgFew : kMxSeqAvg;
+            job.seq_blocks = nnz < (int64_t)job.seq_avg * B ? 0 : (int)((few ? n_bags : std::min<int64_t>(kMxSeqBlocks, nnz / kMxSeqIds + 1)) + 7) / 8 * 8;
             job.fmeta = ds->fmeta; job.ids = ids; job.offsets = offsets; job.out = out; job.out_stride = out_row_stride; job.error_word = error_word;
             PK_LAUNCH("pk_mx_lookup", mx_lookup_kernel, dim3((unsigned)(job.seq_blocks + items)), dim3(64), 0, job);
         }

@@ -82,6 +82,21 @@ def test_long_bags(dim, max_len):
     run(small_problem(max_len + dim, B=11, tables=[(5000, dim, 0), (300, dim, 0)], fields=[(0, 0), (1, 1)], max_len=max_len))
 
 
+@pytest.mark.parametrize("dim", [5, 8, 16, 20, 32, 64, 96, 200])
+@pytest.mark.parametrize("B,max_len", [(5000, 1), (4100, 2), (2100, 40), (2100, 9)])
+def test_large_batches(B, max_len, dim):
+    """(more bags than get a wavefront each, and one-hot bags that are written by tiles)"""
+    run(small_problem(B + dim, B=B, tables=[(3000, dim, 0), (77, dim, 0)], fields=[(0, 0), (1, 1)], max_len=max_len, allow_empty=max_len > 1), pad=1)
+
+
+@pytest.mark.parametrize("B,F", [(1, 1), (1, 26), (4, 9), (4096, 1), (4097, 1)])
+@pytest.mark.parametrize("max_len", [12, 20, 60])
+def test_few_bags(B, F, max_len):
+    """(up to 4096 bags of eight IDs and more have a wavefront each)"""
+    tables = [(500 + f, (32, 8, 64, 16, 128, 3)[f % 6], 0) for f in range(F)]
+    run(small_problem(B + max_len, B=B, tables=tables, fields=[(f, f % 2) for f in range(F)], max_len=max_len))
+
+
 def test_long_and_short_fields_together():
     tables = [(400, 16, 0), (900, 64, 0), (50, 8, 0)]
     fields = [(0, 0), (1, 1), (2, 0), (1, 0), (0, 1)]
