@@ -324,7 +324,7 @@ pk_status pk_partition_unique(const pk_plan* plan, const void* workspace, size_t
  * (pk_mx_weight_grad: the sum over no samples).  These calls need no plan, allocate
  * nothing and only enqueue work on hip_stream, which belongs to the current device;
  * workspaces are the caller's, and calls that may run at the same time (two streams,
- * two graphs) need one each. */
+ * two graphs) need one each.  What a call writes overlaps nothing that it reads. */
 size_t    pk_mx_row_bytes(int32_t format, int64_t cols);   /* 0: unknown format or bad cols */
 /* src: device, fp32 or bf16 [n_rows, src_row_stride]; rows: device, out. */
 pk_status pk_mx_quantize(const void* src, int32_t src_dtype, int64_t src_row_stride, int64_t n_rows, int64_t cols,
@@ -340,10 +340,13 @@ pk_status pk_mx_dequantize(const void* rows, int64_t row_stride, int64_t n_rows,
  *           stacked table, total_rows rows of PK_MXFP4 with row_stride =
  *           pk_mx_row_bytes(PK_MXFP4, dim).  The plan's dtypes say what the tables were
  *           rounded from.
- * ids, offsets, out: as for pk_forward; sums are kept in double, the mean's division too.
+ * ids, offsets, out: as for pk_forward; sums are kept in double (where bags are long, of up to
+ *           eight rows added in fp32), the mean's division too.
  * error_word: device, int32.  Offsets that violate the contract raise bit 0 (OR: the
  *           caller clears it); a bag that begins before 0, ends before it begins or
- *           behind nnz pools to zeros, nothing is read for it, and the others are pooled. */
+ *           behind nnz pools to zeros, nothing is read for it, and the others are pooled.
+ * A plan's first call on a GPU (of any kind) allocates and copies the plan's metadata
+ * there: before a graph is captured, not into it.  Calls on one plan may run side by side. */
 pk_status pk_mx_forward(const pk_plan* plan, const void* const* T, const int64_t* ids, const int32_t* offsets,
                         int32_t B, int64_t nnz, float* out, int64_t out_row_stride, int32_t* error_word,
                         void* hip_stream);
@@ -363,7 +366,8 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
 
 /* The gradient of a dense layer's weights from the 8-bit checkpoint of its input:
  *   dw[n, k] (+)= sum_b dy[b, n] * X[b, k]
- * dy: device, fp32 or bf16 [B, dy_row_stride], N and the stride at most 2^24 (fp32 numbers are multiplied in full);
+ * dy: device, fp32 or bf16 [B, dy_row_stride], N and the stride at most 2^24 (fp32 numbers are
+ * multiplied in full, digits below 2^-133 aside);
  * x_rows: device, B rows of K columns, PK_MXFP8;  dw: device, fp32 [N, dw_row_stride].
  * accumulate: 0 = dw is overwritten, else added to (micro-batches).  Sums in fp32, in an
  * order that depends on the sizes only: the same call gives the same bits.

@@ -5,8 +5,8 @@
 // The sum runs over the samples, which are the rows of both operands, while a lane of a matrix instruction wants eight
 // consecutive samples of one column: a thread loads eight rows of four columns, and turns them over in registers on the way to
 // LDS.  X's elements become bf16 there (four digits and a power of two: exact); of an fp32 dY every element becomes three
-// bf16 numbers whose sum it is (8 + 8 + 8 digits, cut off, not rounded), so that all products are exact and what is
-// lost is what fp32 additions lose.
+// bf16 numbers whose sum it is (8 + 8 + 8 digits, cut off, not rounded; digits below 2^-133, the smallest bf16 number, are
+// lost), so that all products are exact and what is lost is what fp32 additions lose.
 // A block takes kGradN x kGradK elements of dW and a stretch of the samples, kGradB a step; the stretches' sums meet in a
 // second launch in their order, so that a result does not depend on which block came first.
 // ---------------------------------------------------------------------------
@@ -238,7 +238,10 @@ mx_grad_f32_kernel(GradJob g)
             for (int p = 0; p < 3; ++p) {                  // the upper half of what is left: its next eight digits
                 fa[p] = __builtin_bit_cast(bf16x8, grad_turn(a[kk][0], a[kk][1], a[kk][2], a[kk][3], a[kk][4], a[kk][5], a[kk][6], a[kk][7], kHighHalves));
 #pragma unroll
-                for (int i = 0; i < 8 && p < 2; ++i) a[kk][i] = __float_as_uint(__uint_as_float(a[kk][i]) - __uint_as_float(a[kk][i] & 0xFFFF0000u));
+                for (int i = 0; i < 8 && p < 2; ++i) {
+                    const float v = __uint_as_float(a[kk][i]), rest = v - __uint_as_float(a[kk][i] & 0xFFFF0000u);
+                    a[kk][i] = __float_as_uint(p == 0 && __builtin_isinf(v) ? 0.f : rest);   // (nothing is left of an infinity)
+                }
             }
             if (more) load(step + 1, kk);
 #pragma unroll
