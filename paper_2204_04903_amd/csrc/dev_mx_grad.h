@@ -9,9 +9,12 @@
 // lost), so that all products are exact and what is lost is what fp32 additions lose.
 // A block takes kGradN x kGradK elements of dW and a stretch of the samples, kGradB a step; the stretches' sums meet in a
 // second launch in their order, so that a result does not depend on which block came first.
+// bf16, 8192 samples, 832 x 1024: 32 us (0.43 PFLOP/s: turning over and LDS, the matrix unit would take 10) and 6.4 to join nine
+// stretches.  fp32, 512 samples, 12000 x 1024, added to dW: 51 us (0.73 PFLOP/s of bf16 products).
 // ---------------------------------------------------------------------------
 constexpr int kGradN = 128, kGradK = 128, kGradB = 64;
-constexpr int64_t kGradBlocks = 512;             // two blocks a compute unit
+// Blocks that the stretches are cut for, two a compute unit: 8192 samples, 832 x 1024, bf16, 39.9 us; 256 blocks 47.8, one stretch 140.
+constexpr int64_t kGradBlocks = 512;
 constexpr int kGradRow = kGradB * 2;             // bytes of a column's samples in LDS
 
 struct GradLayout { int64_t tiles_n, tiles, steps, splits, ld; size_t total; };
@@ -135,7 +138,8 @@ __device__ __forceinline__ void grad_write(const GradJob& g, const GradWork& w, 
 }
 
 // dY in bf16: both operands by way of LDS, a wavefront takes 64 x 64.  A step on its way while one is multiplied; the other block
-// of the compute unit fills the pauses.
+// of the compute unit fills the pauses.  (dY from memory to registers, as below, takes 46.9 us instead of 40.5 with the joining: with one
+// product instead of three for what a lane has read, its loads are what is waited for.)
 __global__ void __launch_bounds__(256, 2)
 mx_grad_bf16_kernel(GradJob g)
 {

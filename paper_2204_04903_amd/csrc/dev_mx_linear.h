@@ -8,11 +8,16 @@
 // lane 16 bytes and a scale: row (column) l % 16 and of the 128 the block l / 16.  W is its first operand, so that a lane's four results are
 // neighbours in a row of y.  Where the tiles are too few for the chip, K is cut into stretches whose sums meet in a second
 // launch, in their order.
+// 2048 x 12000 -> 1024: rounding 18 us (98 MB read: 5.5 TB/s), product 27 (1.9 PFLOP/s: a step's stores to LDS and its barriers, not
+// the matrix unit), joining four stretches 9.  8192 x 832 -> 1024: rounding 7.1, product 15.7 (four steps a tile: its first loads and
+// 17 MB of y).
 // ---------------------------------------------------------------------------
 constexpr int kLinM = 128, kLinN = 128, kLinK = 256;
 constexpr int kLinRow = kLinK / 2;               // bytes of a row's codes in LDS
 constexpr int kLinScales = 16;                   // steps whose scales are in LDS at a time: 128 bytes a row
-constexpr int kLinStretch = 6;                   // steps of a stretch, at least
+// Steps of a stretch, at least: its tile is written and read once more.  2048 x 12000 -> 1024 takes 53 us in four stretches and 68 in one,
+// 512 x 12000 -> 256 23 and 54; stretches of two steps cost 2048 x 2048 -> 1024 26 us instead of 18.
+constexpr int kLinStretch = 6;
 
 // Few rows of x, up to 16 of kLinFew elements together, take one launch (K 832, N 1024, 1 and 16 rows: 4.2 and 5.1 us, by tiles 10.5 and
 // 10.8; K 3840, 16 rows 10.7 and 15.0; K 6000 and 16 rows 15.3 both; K 12000, N 1024, 1, 4, 8 rows 13.8 17.7 21.5, by tiles 16.3 16.4 16.7:

@@ -15,6 +15,8 @@
 // scales are far apart), the rounds in double.  Fields of sequences (kMxSeqAvg IDs per bag on average and more) go to
 // wavefronts of their own, which start first: there the groups of a wavefront share a bag, and their sums meet by halves, every
 // lane giving away half of its columns a step.
+// 200 fields of 8 to 64 columns, 20.9 M IDs: 217 to 226 us, 93 to 96 G rows/s (when it took 240: 135 with all rows in the L2s, 185 without the
+// output's writes); 10 sequence fields of 100 to 1000 IDs, 64 columns, 1024 samples: 57 us, 99 G; 26 one-hot fields, 64 samples: 5.
 // ---------------------------------------------------------------------------
 constexpr int kMxPacks = 16;     // packs of one launch
 // From which average a field's bags go to wavefronts of their own, by the number of bags.  Few bags are too few tiles for the chip: one sample
@@ -22,8 +24,8 @@ constexpr int kMxPacks = 16;     // packs of one launch
 // fields 13.0 and 12.7 at 8, 27 and 13.4 at 50.  Many keep the tiles busy: 1024 samples of 26 fields 32.8 and 56 at 63 IDs a bag.
 constexpr int kMxSeqAvg = 64, kMxSeqAvgFew = 8;
 constexpr int64_t kMxFewBags = 4096;
-constexpr int64_t kMxSeqBlocks = 8192, kMxSeqIds = 512;      // wavefronts for their bags, at most, and IDs that there should be for each
-constexpr int kMxXcdFields = 32; // fields from which every one has its XCD
+constexpr int64_t kMxSeqBlocks = 8192, kMxSeqIds = 512;      // wavefronts for their bags, at most (half as many: sequences of 550 IDs 63 us instead of 57), and IDs that there should be for each
+constexpr int kMxXcdFields = 32; // fields from which every one has its XCD: 8192 samples of 32 fields 24.1 us so and 28.1 without, of 64 39.4 and 47.4
 // One-hot bags of this many samples and more are written by tiles too: 26 fields of 32 columns, 8192 samples, 17.2 us bag by bag, 15.3 so;
 // 100 of 16 columns and 2 IDs, 1024 samples, 10.2 and 10.9; 26 of 32, 64 samples, 4.8 and 5.6.
 constexpr int kMxStagedBags = 4096;
@@ -416,6 +418,8 @@ mx_lookup_kernel(MxJob job)
     const FieldMeta m = as_global(job.fmeta)[f];
 #define MX_TILE8(K) mx_tile<K, 8>(job, k, m, offs, tile, s_bin, s_bag, s_key, s_out)
 #define MX_TILE1(K) mx_tile<K, 1>(job, k, m, offs, tile, s_bin, s_bag, s_key, s_out)
+    // (rounds of eight rows from two and a half IDs a bag on: 40 fields of 64 columns, 2048 samples, 3 IDs a bag 14.1 us so and 16.4 row by
+    // row, 6 15.2 and 20.1; 100 of 16 columns 17.1 and 15.9 at 3, 21.8 both at 6)
     if (2 * field_ids > 5 * (int64_t)job.B) { MX_KINDS(MX_TILE8) }
     else { MX_KINDS(MX_TILE1) }
 }
