@@ -306,7 +306,9 @@ pk_status pk_partition_unique(const pk_plan* plan, const void* workspace, size_t
  * shorter).  A block has one scale 2^t, t the smallest integer, -126 at least, with
  * which the block's largest magnitude is at most 2^t times the format's largest
  * value; its elements divided by 2^t are rounded to the nearest value of the format,
- * ties to the even code, so that an element of a block is off by at most half a step:
+ * ties to the even code, so that an element of a block is off by at most half a step
+ * (finite numbers stay finite: what is nearest to 2^128 is held as the value below, 1.5 * 2^127
+ * in 4 bits, 1.875 * 2^127 in 8, off by less than 2^-2 and 2^-4 of itself):
  *   PK_MXFP4  E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; two columns a byte, the
  *             lower column in the lower bits
  *   PK_MXFP8  E4M3: sign, four exponent and three mantissa bits, up to 448; a byte each
@@ -330,7 +332,7 @@ size_t    pk_mx_row_bytes(int32_t format, int64_t cols);   /* 0: unknown format 
 pk_status pk_mx_quantize(const void* src, int32_t src_dtype, int64_t src_row_stride, int64_t n_rows, int64_t cols,
                          int32_t format, void* rows, int64_t row_stride, void* hip_stream);
 /* dst: device, fp32 or bf16 [n_rows, dst_row_stride], columns [0, cols) are written.
- * Both types hold every value of both formats exactly (bf16: from 2^-133 on). */
+ * Both types hold every value that pk_mx_quantize writes exactly (bf16: from 2^-133 on). */
 pk_status pk_mx_dequantize(const void* rows, int64_t row_stride, int64_t n_rows, int64_t cols, int32_t format,
                            void* dst, int32_t dst_dtype, int64_t dst_row_stride, void* hip_stream);
 

@@ -33,7 +33,7 @@ def nearest(u, fmt):
 
 
 def encode(x, fmt):
-    """x [R, C] -> uint8 [R, row_bytes]"""
+    """x [R, C] -> uint8 [R, row_bytes]; what is nearest to 2^128, past fp32's range, gets the code below"""
     x = np.asarray(x, np.float64)
     R, C = x.shape
     n = code_bytes(fmt, C)
@@ -45,7 +45,9 @@ def encode(x, fmt):
         t = scale_exponent(np.where(bad, 1.0, np.abs(v).max(1)), fmt)
         out[:, n + b] = np.where(bad, 255, t + 127)
         u = np.where(bad[:, None], 0.0, np.abs(v)) / 2.0 ** t[:, None].astype(np.float64)
-        c = nearest(u, fmt) | np.signbit(v).astype(np.int64) << (3 if fmt == MXFP4 else 7)
+        c = nearest(u, fmt)
+        c = np.where(GRID[fmt][c] * 2.0 ** t[:, None].astype(np.float64) >= 2.0 ** 128, c - 1, c)
+        c = c | np.signbit(v).astype(np.int64) << (3 if fmt == MXFP4 else 7)
         codes[:, 32 * b:32 * b + v.shape[1]] = np.where(bad[:, None], 0 if fmt == MXFP4 else 0x7F, c)
     if fmt == MXFP4:
         codes = codes[:, 0::2] | codes[:, 1::2] << 4

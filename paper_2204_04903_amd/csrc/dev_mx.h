@@ -3,8 +3,9 @@
 
 // ---------------------------------------------------------------------------
 // A block of 32 columns with largest magnitude m has the scale 2^t, t the smallest integer with m <= MAX * 2^t (MAX: 6 of
-// E2M1, 448 of E4M3), so that nothing saturates and every element is off by at most half a step of its format; the
-// scale byte is t + 127, from 1 (2^-126, also of a block of zeros) on.  A block that holds an infinity or a NaN has the
+// E2M1, 448 of E4M3), so that every element is off by at most half a step of its format; the scale byte is t + 127, from 1
+// (2^-126, also of a block of zeros) on.  One code is not used: what is nearest to 2^128, which fp32 does not hold, gets the
+// code below (1.5 and 1.875 times 2^127), still within 2^-2 and 2^-4 of itself.  A block that holds an infinity or a NaN has the
 // scale byte 255 and reads back as NaN.  (With the other usual rule, t = floor(log2 m) less the exponent of MAX, the
 // elements between MAX and the next power of two saturate: 32 normal columns in 8 bits 2.9 % off instead of 2.7, in 4 bits 11.5 both.)
 // ---------------------------------------------------------------------------
@@ -17,6 +18,9 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t max_bits)       // bi
                                   : e - 8 + (m > 0x600000);                // 448 = 1.75 * 2^8
     return (uint32_t)max(t, 1);
 }
+// the scale byte of the blocks that hold numbers so large, and the largest that is held
+template <int FMT> constexpr uint32_t kMxTopByte = FMT == PK_MXFP4 ? 126 + 127 : 120 + 127;
+template <int FMT> constexpr float kMxTop = FMT == PK_MXFP4 ? 0x1.8p127f : 0x1.Ep127f;
 // the scale as the number that the conversions take (they read its exponent; byte 255: NaN)
 __device__ __forceinline__ float mx_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
@@ -26,9 +30,16 @@ typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 
 // eight columns of a block, first column in the lowest bits
 template <int FMT>
-__device__ __forceinline__ void mx_encode8(const float (&x)[8], uint32_t byte, uint32_t (&w)[FMT == PK_MXFP4 ? 1 : 2])
+__device__ __forceinline__ void mx_encode8(const float (&v)[8], uint32_t byte, uint32_t (&w)[FMT == PK_MXFP4 ? 1 : 2])
 {
     const float s = mx_scale(byte);
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = v[i];
+    if (byte == kMxTopByte<FMT>) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_fmed3f(x[i], -kMxTop<FMT>, kMxTop<FMT>);
+    }
     if constexpr (FMT == PK_MXFP4) {
         uint32_t u = 0;
         u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[0], x[1], s, 0);
