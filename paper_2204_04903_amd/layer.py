@@ -284,20 +284,21 @@ class QuantizedLinear:
         dense = QuantizedLinear(weight, bias)            # weight: fp32 or bf16 [N, K]; bias: fp32 [N] or None
         y = dense.forward(out)                           # out: fp32 or bf16 [M, K]; y: fp32, or dtype=torch.bfloat16
 
-    `weight` may be an MxRows of PK_MXFP4 rows instead (copied where its rows do not begin on 128-byte lines).  Buffer management only."""
+    `weight` may be an MxRows of PK_MXFP4 rows instead.  The layer keeps the weights in rows of its own, `dense.weight`, that begin on
+    128-byte lines: what is written to `weight` later does not change it, `dense.weight.quantize(...)` does.  Buffer management only."""
 
     def __init__(self, weight, bias: torch.Tensor = None):
-        if not isinstance(weight, MxRows):
-            weight = MxRows(weight.shape[0], weight.shape[1], pk.PK_MXFP4, device=weight.device, align=128).quantize(weight)
-        if weight.format != pk.PK_MXFP4:
+        if isinstance(weight, MxRows) and weight.format != pk.PK_MXFP4:
             raise ValueError("weight rows must be PK_MXFP4")
-        if weight.stride % 128 or weight.data.data_ptr() % 128:      # whole lines a row: what the product reads of one is what it needs
-            laid = MxRows(weight.n_rows, weight.cols, weight.format, device=weight.device, align=128)
-            need = pk.pk_mx_row_bytes(weight.format, weight.cols)
-            laid.data[:, :need].copy_(weight.data[:, :need])
-            weight = laid
-        self.weight, self.device = weight, weight.device
-        self.N, self.K = weight.n_rows, weight.cols
+        self.N, self.K = (weight.n_rows, weight.cols) if isinstance(weight, MxRows) else (int(n) for n in weight.shape)
+        # (whole lines a row: what the product reads of one is what it needs)
+        self.weight = MxRows(self.N, self.K, pk.PK_MXFP4, device=weight.device, align=128)
+        self.device = self.weight.device
+        if isinstance(weight, MxRows):
+            need = pk.pk_mx_row_bytes(pk.PK_MXFP4, self.K)
+            self.weight.data[:, :need].copy_(weight.data[:, :need])
+        else:
+            self.weight.quantize(weight)
         if bias is not None and (bias.dtype != torch.float32 or bias.shape != (self.N,) or bias.device != self.device or
                                  (self.N > 1 and bias.stride(0) != 1)):
             raise ValueError(f"bias must be fp32 [{self.N}], contiguous, on {self.device}")
