@@ -333,6 +333,13 @@ class QuantizedEmbedding:
         self.tables, self.fields = list(tables), list(fields)
         self.device = _device(device)
         self.plan = pk.pk_plan_create(self.tables, self.fields, **plan_opts)
+        try:
+            self._hold(rows)
+        except BaseException:
+            self.close()                                     # (nobody else can: the caller gets no object)
+            raise
+
+    def _hold(self, rows) -> None:
         self.n_packs = pk.pk_plan_num_packs(self.plan)
         self.packs = [pk.pk_plan_pack_info(self.plan, p) for p in range(self.n_packs)]
         self.table_slot = [pk.pk_plan_table_slot(self.plan, t) for t in range(len(self.tables))]
@@ -355,10 +362,14 @@ class QuantizedEmbedding:
         if isinstance(layer, HybridEmbedding):
             raise ValueError("rows in a Hot-storage are newer than the tables: quantize a PackedEmbedding")
         q = cls(layer.tables, layer.fields, device=layer.device, **plan_opts)
-        if [(k["dim"], k["dtype"], k["total_rows"]) for k in q.packs] != [(k["dim"], k["dtype"], k["total_rows"]) for k in layer.packs]:
-            raise ValueError("the layer was made with other plan options")
-        for t in range(len(q.tables)):
-            q.load_table(t, layer.table_view(t))
+        try:
+            if [(k["dim"], k["dtype"], k["total_rows"]) for k in q.packs] != [(k["dim"], k["dtype"], k["total_rows"]) for k in layer.packs]:
+                raise ValueError("the layer was made with other plan options")
+            for t in range(len(q.tables)):
+                q.load_table(t, layer.table_view(t))
+        except BaseException:
+            q.close()
+            raise
         return q
 
     def close(self):
