@@ -394,10 +394,13 @@ class QuantizedEmbedding:
         return out
 
     def error_word(self) -> int:
-        """Bit 0: some call's offsets were rejected since the word was last read (reading clears it; synchronises)."""
+        """Bit 0: some call's offsets were rejected since the word was last read (reading clears it).  Synchronises the device, whatever
+        streams the calls were on, and is not to be called while another thread makes some."""
+        torch.cuda.synchronize(self.device)
         w = int(self.error.item())
         if w:
             self.error.zero_()
+            torch.cuda.synchronize(self.device)              # (a call that follows on another stream may raise it again)
         return w
 
 
