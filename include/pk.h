@@ -322,7 +322,8 @@ pk_status pk_partition_unique(const pk_plan* plan, const void* workspace, size_t
  *
  * Matrices of fp32 or bf16: element-aligned, row stride in elements, >= the columns
  * (not looked at for one row).  Sizes below 2^31; of products at
- * most 2^30, K at most 2^23 and the microscaled rows at most 2^24 bytes apart.  Calls with no rows do nothing
+ * most 2^30, K at most 2^23, the microscaled rows at most 2^24 bytes apart and the result at most 2^24 - 8
+ * pieces of 128 x 128 (the last ones of a row and a column may be smaller).  Calls with no rows do nothing
  * (pk_mx_weight_grad: the sum over no samples).  These calls need no plan, allocate
  * nothing and only enqueue work on hip_stream, which belongs to the current device;
  * workspaces are the caller's, and calls that may run at the same time (two streams,

@@ -23,7 +23,11 @@ constexpr int kLinStretch = 6;
 // 10.8; K 3840, 16 rows 10.7 and 15.0; K 6000 and 16 rows 15.3 both; K 12000, N 1024, 1, 4, 8 rows 13.8 17.7 21.5, by tiles 16.3 16.4 16.7:
 // each block reads all of x).
 constexpr int64_t kLinFew = 1 << 16;
-inline bool linear_few(int64_t M, int64_t K) { return M <= 16 && M * K <= kLinFew; }
+inline int linear_few_waves(int64_t K) { return (int)std::min<int64_t>(16, std::max<int64_t>(1, (K + 255) / 256)); }
+inline bool linear_few(int64_t M, int64_t N, int64_t K)
+{
+    return M <= 16 && M * K <= kLinFew && (N + 15) / 16 * (64 * linear_few_waves(K)) < kLaunchThreads;
+}
 struct LinearLayout { int64_t kp, tiles_m, tiles_n, steps, splits, ld; size_t scales, parts, total; };
 inline LinearLayout linear_layout(int64_t M, int64_t N, int64_t K)
 {
@@ -38,7 +42,7 @@ inline LinearLayout linear_layout(int64_t M, int64_t N, int64_t K)
     L.ld = (N + 3) / 4 * 4;
     L.scales = pad(M * (L.kp / 2));
     L.parts = L.scales + pad(M * (L.kp / 32));
-    L.total = linear_few(M, K) ? kAlign : std::max<size_t>(kAlign, L.parts + (L.splits > 1 ? pad(L.splits * M * L.ld * 4) : 0));
+    L.total = linear_few(M, N, K) ? kAlign : std::max<size_t>(kAlign, L.parts + (L.splits > 1 ? pad(L.splits * M * L.ld * 4) : 0));
     return L;
 }
 

@@ -19,6 +19,8 @@ struct RowGroups {                   // a row's groups of eight columns, whole b
         return row0 + dr;
     }
 };
+// a launch has fewer threads than this; blocks of 256, dealt out in eights
+constexpr int64_t kLaunchThreads = (int64_t)1 << 32, kLaunchBlocks = kLaunchThreads / 256 - 8;
 inline unsigned mx_blocks_for(int64_t items)
 {
     return (unsigned)std::min<int64_t>((items + NT - 1) / NT, (int64_t)1 << 20);

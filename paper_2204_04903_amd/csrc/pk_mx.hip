@@ -172,8 +172,8 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
         if (ws_bytes < L.total) return fail(PK_EWORKSPACE, std::string(who) + ": workspace is smaller than pk_mx_linear_workspace_bytes");
         hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         const int64_t x_bytes = x_row_stride * (x_dtype == PK_BF16 ? 2 : 4);
-        if (linear_few(M, K)) {
-            const int waves = (int)std::min<int64_t>(16, std::max<int64_t>(1, (K + 255) / 256));
+        if (linear_few(M, N, K)) {
+            const int waves = linear_few_waves(K);
             const auto few = x_dtype == PK_BF16 ? (y_dtype == PK_BF16 ? mx_linear_few_kernel<true, true> : mx_linear_few_kernel<true, false>)
                                                 : (y_dtype == PK_BF16 ? mx_linear_few_kernel<false, true> : mx_linear_few_kernel<false, false>);
             MX_LAUNCH("mx_linear_few", few, dim3((unsigned)((N + 15) / 16)), dim3(64 * waves), static_cast<const char*>(x), x_bytes, (int)M,
@@ -183,7 +183,7 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
         char* ws = static_cast<char*>(workspace);
         const RowGroups g(L.kp);
         const int64_t items = M * g.n, tiles = L.tiles_m * L.tiles_n;
-        if (tiles * L.splits > ((int64_t)1 << 30)) return fail(PK_EOVERFLOW, std::string(who) + ": M * N is too large");
+        if (tiles * L.splits > kLaunchBlocks) return fail(PK_EOVERFLOW, std::string(who) + ": M * N is too large");
         uint32_t* codes = reinterpret_cast<uint32_t*>(ws);
         uint8_t* scales = reinterpret_cast<uint8_t*>(ws + L.scales);
         const auto round = x_dtype == PK_BF16 ? mx_linear_round_kernel<true> : mx_linear_round_kernel<false>;
@@ -230,7 +230,7 @@ pk_status pk_mx_weight_grad(const void* dy, int32_t dy_dtype, int64_t dy_row_str
         hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         const GradLayout L = grad_layout(B, N, K);
         const int64_t tiles = L.tiles;
-        if (tiles * L.splits > ((int64_t)1 << 30)) return fail(PK_EOVERFLOW, std::string(who) + ": N * K is too large");
+        if (tiles * L.splits > kLaunchBlocks) return fail(PK_EOVERFLOW, std::string(who) + ": N * K is too large");
         const bool join = L.splits > 1;
         const GradJob job{static_cast<const char*>(dy), (B > 1 ? dy_row_stride : N) * (dy_dtype == PK_BF16 ? 2 : 4), static_cast<const uint8_t*>(x_rows), x_row_stride, B,
                           (int)N, (int)K, (int)L.tiles_n, (int)tiles, (int)L.steps, (int)L.splits, join ? static_cast<float*>(workspace) : dw,
