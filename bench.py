@@ -304,7 +304,7 @@ def run_workload(args, workload):
     if layer.error_word() != 0:
         raise RuntimeError(f"{workload}: the device error word is {layer.error_word()} after the timed steps")
 
-    # ---- Partition of the last step's distinct keys (outside the timed steps) ----------------------
+    # ---- the batches' lookups from 4-bit copies of the tables (outside the timed steps) -------------
     serve_info = None
     if args.serve_4bit and not hybrid:
         from paper_2204_04903_amd.layer import QuantizedEmbedding
@@ -328,6 +328,7 @@ def run_workload(args, workload):
                       "full_table_bytes": sum(int(w.numel()) * w.element_size() for w in layer.W), "error_word": serve.error_word()}
         serve.close()
 
+    # ---- Partition of a step's distinct keys (outside the timed steps) ------------------------------
     partition_info = None
     if args.partition > 0 and not hybrid:
         n_own = args.partition

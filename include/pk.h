@@ -370,7 +370,7 @@ pk_status pk_mx_linear(const void* x, int32_t x_dtype, int64_t x_row_stride, int
 /* The gradient of a dense layer's weights from the 8-bit checkpoint of its input:
  *   dw[n, k] (+)= sum_b dy[b, n] * X[b, k]
  * dy: device, fp32 or bf16 [B, dy_row_stride], N and the stride at most 2^24 (fp32 numbers are
- * multiplied in full, digits below 2^-133 aside);
+ * multiplied in full; digits of theirs and elements of X below 2^-133, bf16's smallest number, are lost);
  * x_rows: device, B rows of K columns, PK_MXFP8;  dw: device, fp32 [N, dw_row_stride].
  * accumulate: 0 = dw is overwritten, else added to (micro-batches).  Sums in fp32, in an
  * order that depends on the sizes only: the same call gives the same bits.

@@ -4,13 +4,13 @@
 // ---------------------------------------------------------------------------
 // The sum runs over the samples, which are the rows of both operands, while a lane of a matrix instruction wants eight
 // consecutive samples of one column: a thread loads eight rows of four columns, and turns them over in registers on the way to
-// LDS.  X's elements become bf16 there (four digits and a power of two: exact); of an fp32 dY every element becomes three
-// bf16 numbers whose sum it is (8 + 8 + 8 digits, cut off, not rounded; digits below 2^-133, the smallest bf16 number, are
-// lost), so that all products are exact and what is lost is what fp32 additions lose.
+// LDS.  X's elements become bf16 there (four digits and a power of two: exact, from 2^-133 on, the smallest bf16 number); of an
+// fp32 dY every element becomes three bf16 numbers whose sum it is (8 + 8 + 8 digits, cut off, not rounded; digits below
+// 2^-133 are lost), so that all products are exact and what is lost is what fp32 additions lose.
 // A block takes kGradN x kGradK elements of dW and a stretch of the samples, kGradB a step; the stretches' sums meet in a
 // second launch in their order, so that a result does not depend on which block came first.
-// bf16, 8192 samples, 832 x 1024: 32 us (0.43 PFLOP/s: turning over and LDS, the matrix unit would take 10) and 6.4 to join nine
-// stretches.  fp32, 512 samples, 12000 x 1024, added to dW: 51 us (0.73 PFLOP/s of bf16 products).
+// bf16, 8192 samples, 832 x 1024: 29 us (0.48 PFLOP/s: narrow loads, turning over and LDS, the matrix unit would take 10) and 6.3 to
+// join nine stretches.  fp32, 512 samples, 12000 x 1024, added to dW: 45 us (0.84 PFLOP/s of bf16 products).
 // ---------------------------------------------------------------------------
 constexpr int kGradN = 128, kGradK = 128, kGradB = 64;
 // Blocks that the stretches are cut for, two a compute unit: 8192 samples, 832 x 1024, bf16, 39.9 us; 256 blocks 47.8, one stretch 140.

@@ -8,9 +8,9 @@
 // lane 16 bytes and a scale: row (column) l % 16 and of the 128 the block l / 16.  W is its first operand, so that a lane's four results are
 // neighbours in a row of y.  Where the tiles are too few for the chip, K is cut into stretches whose sums meet in a second
 // launch, in their order.
-// 2048 x 12000 -> 1024: rounding 18 us (98 MB read: 5.5 TB/s), product 27 (1.9 PFLOP/s: a step's stores to LDS and its barriers, not
-// the matrix unit), joining four stretches 9.  8192 x 832 -> 1024: rounding 7.1, product 15.7 (four steps a tile: its first loads and
-// 17 MB of y).
+// 2048 x 12000 -> 1024: rounding 17.5 us (98 MB read, 13 written: 6.3 TB/s), product 24.6 (2.0 PFLOP/s: a step's stores to LDS and its
+// barriers, not the matrix unit), joining four stretches 9.2.  8192 x 832 -> 1024: rounding 7.0, product 14.7 (four steps a tile: its first
+// loads and 17 MB of y).
 // ---------------------------------------------------------------------------
 constexpr int kLinM = 128, kLinN = 128, kLinK = 256;
 constexpr int kLinRow = kLinK / 2;               // bytes of a row's codes in LDS

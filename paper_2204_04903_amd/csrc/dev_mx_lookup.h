@@ -15,17 +15,24 @@
 // scales are far apart), the rounds in double.  Fields of sequences (kMxSeqAvg IDs per bag on average and more) go to
 // wavefronts of their own, which start first: there the groups of a wavefront share a bag, and their sums meet by halves, every
 // lane giving away half of its columns a step.
-// 200 fields of 8 to 64 columns, 20.9 M IDs: 217 to 226 us, 93 to 96 G rows/s (when it took 240: 135 with all rows in the L2s, 185 without the
-// output's writes); 10 sequence fields of 100 to 1000 IDs, 64 columns, 1024 samples: 57 us, 99 G; 26 one-hot fields, 64 samples: 5.
+// 200 fields of 8 to 64 columns, 20.9 M IDs: 215 us, 97 G rows/s, 763 MB past the L2s (an earlier form took 240: 135 with all rows in the
+// L2s, 185 without the output's writes); 10 sequence fields of 100 to 1000 IDs, 64 columns, 1024 samples: 53 us, 107 G; 26 one-hot
+// fields, 64 samples: 5.
 // ---------------------------------------------------------------------------
 constexpr int kMxPacks = 16;     // packs of one launch
 // From which average a field's bags go to wavefronts of their own, by the number of bags.  Few bags are too few tiles for the chip: one sample
 // of 26 fields of 32 columns takes 5.6 us at 6 IDs a bag by tiles and 5.7 by bags, 6.7 and 6.0 at 8, 12.6 and 6.1 at 50; 128 samples of 30
-// fields 13.0 and 12.7 at 8, 27 and 13.4 at 50.  Many keep the tiles busy: 1024 samples of 26 fields 32.8 and 56 at 63 IDs a bag.
+// fields 13.0 and 12.7 at 8, 27 and 13.4 at 50.  Many keep the tiles busy: 1024 samples of 26 fields 32.8 and 56 at 63 IDs a bag.  Where the two
+// meet depends on more than the bags: 30 fields of 50 IDs take 28.7 by tiles and 13.1 by bags with 4110 bags, 31.2 and 20.4 with 7680, 32.8 and
+// 36.6 with 15 360 (of 25 IDs 17.3 and 12.7, 18.0 and 19.0, 21.0 and 36.0); 200 fields of 25 IDs 17.0 and 73 with 12 800, since every wavefront
+// walks the list of fields.  It is a field's average that counts: a long bag among short ones is one lane group's.
 constexpr int kMxSeqAvg = 64, kMxSeqAvgFew = 8;
 constexpr int64_t kMxFewBags = 4096;
 constexpr int64_t kMxSeqBlocks = 8192, kMxSeqIds = 512;      // wavefronts for their bags, at most (half as many: sequences of 550 IDs 63 us instead of 57), and IDs that there should be for each
-constexpr int kMxXcdFields = 32; // fields from which every one has its XCD: 8192 samples of 32 fields 24.1 us so and 28.1 without, of 64 39.4 and 47.4
+// Fields from which every one has its XCD.  8192 samples, 32 columns, 5 IDs: 32 fields 22.7 us so and 26.8 without, 33 25.2 and 27.6, 41 30.9 and 33.6, 64
+// 37.4 and 45.4.  3001 samples of four widths, where the XCDs' shares are less even: 32 fields 15.9 and 20.0, 33 19.1 and 20.3, 37 21.4 and 20.7, 41 22.0
+// both, 64 27.3 and 30.1; bags of 0 to 19 IDs in 37 fields 30.0 and 28.5.
+constexpr int kMxXcdFields = 32;
 // One-hot bags of this many samples and more are written by tiles too: 26 fields of 32 columns, 8192 samples, 17.2 us bag by bag, 15.3 so;
 // 100 of 16 columns and 2 IDs, 1024 samples, 10.2 and 10.9; 26 of 32, 64 samples, 4.8 and 5.6.
 constexpr int kMxStagedBags = 4096;

@@ -4,7 +4,7 @@
 // ---------------------------------------------------------------------------
 // A thread takes eight columns, so that a block of 32 is four neighbouring lanes: the largest magnitude of the block is two
 // exchanges away.  Both kernels move bytes and little else: what bounds them is HBM and the cache behind it.  2048 x 12000 fp32 to 8
-// bits 18.5 us (6.7 TB/s), back to bf16 12.8 (5.8); 1 M x 32 bf16 to 4 bits 19.8 (4.2), back to fp32 25.0 (5.9).
+// bits 18.8 us (6.6 TB/s), back to bf16 12.6 (6.0); 1 M x 32 bf16 to 4 bits 19.7 (4.2), back to fp32 24.2 (6.1).
 // ---------------------------------------------------------------------------
 struct RowGroups {                   // a row's groups of eight columns, whole blocks of four
     uint32_t n, magic;               // magic: floor(2^32 / n) + 1, exact for the quotients below 512 / n that are asked of it
