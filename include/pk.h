@@ -344,7 +344,8 @@ pk_status pk_mx_dequantize(const void* rows, int64_t row_stride, int64_t n_rows,
  *           pk_mx_row_bytes(PK_MXFP4, dim).  The plan's dtypes say what the tables were
  *           rounded from.
  * ids, offsets, out: as for pk_forward; sums are kept in double (where bags are long, of up to
- *           eight rows added in fp32), the mean's division too.
+ *           eight rows added in fp32: past its range they are infinite, also where the mean is not),
+ *           the mean's division too.
  * error_word: device, int32.  Offsets that violate the contract raise bit 0 (OR: the
  *           caller clears it); a bag that begins before 0, ends before it begins or
  *           behind nnz pools to zeros, nothing is read for it, and the others are pooled.

@@ -21,7 +21,7 @@ constexpr int kLinStretch = 6;
 
 // Few rows of x, up to 16 of kLinFew elements together, take one launch (K 832, N 1024, 1 and 16 rows: 4.2 and 5.1 us, by tiles 10.5 and
 // 10.8; K 3840, 16 rows 10.7 and 15.0; K 6000 and 16 rows 15.3 both; K 12000, N 1024, 1, 4, 8 rows 13.8 17.7 21.5, by tiles 16.3 16.4 16.7:
-// each block reads all of x).
+// each block reads all of x).  What would be 2^32 threads and more goes by tiles too.
 constexpr int64_t kLinFew = 1 << 16;
 inline int linear_few_waves(int64_t K) { return (int)std::min<int64_t>(16, std::max<int64_t>(1, (K + 255) / 256)); }
 inline bool linear_few(int64_t M, int64_t N, int64_t K)
