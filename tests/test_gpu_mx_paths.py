@@ -111,7 +111,7 @@ def test_sequences_among_many_fields(B):
     run(with_lengths(pr, {f: (64, 400) for f in (0, 255, 256, 299)}, 4))
 
 
-@pytest.mark.parametrize("place", [0, 1500, 3072])
+@pytest.mark.parametrize("place", [0, 1500, 2048, 4096])
 def test_rejected_offsets_of_dealt_sequences(place):
     """(every read is bounded by nnz)"""
     tables = [(300, 24, 0), (200, 64, 0), (100, 8, 0), (90, 16, 0), (80, 16, 0)]
